@@ -256,6 +256,10 @@ int mrp_build_candidates(mrp_ctx *ctx, void *stream, int B, int K, const int32_t
  *   MRP_FLAG_DRAFT_POS   a draft position >= L: taken as a missing draft
  *   MRP_FLAG_PREFIX_LEN  prefix_len[b] outside [0, max_prefix]: clamped
  *   MRP_FLAG_X_TOK       a recorded token >= V (remask_mode 1): clamped
+ *   MRP_FLAG_POSITION    a row's position outside [0, n_pos) of the rotation table: clamped
+ *   MRP_FLAG_ROWS        cu_rows outside [0, n_rows], decreasing, or more than max_new apart: clamped
+ *   MRP_FLAG_KV_LEN      kv_len[b] outside [0, max_pages * page_size]: clamped
+ *   MRP_FLAG_PAGE        a page number outside [0, n_pages): its positions are neither written nor seen
  * mrp_poll_error waits for `stream` (hipStreamSynchronize: not for use under stream capture), returns the
  * bits set since the last poll (0 = none) and clears them, or a negative status; mrp_last_error then
  * names the conditions. */
@@ -263,6 +267,10 @@ int mrp_build_candidates(mrp_ctx *ctx, void *stream, int B, int K, const int32_t
 #define MRP_FLAG_DRAFT_POS 2
 #define MRP_FLAG_PREFIX_LEN 4
 #define MRP_FLAG_X_TOK 8
+#define MRP_FLAG_POSITION 16
+#define MRP_FLAG_ROWS 32
+#define MRP_FLAG_KV_LEN 64
+#define MRP_FLAG_PAGE 128
 int mrp_poll_error(mrp_ctx *ctx, void *stream);
 
 /* For callers that cannot allocate (code under HIP graph capture, tight serving loops, harnesses
@@ -358,6 +366,114 @@ int mrp_kl_loss(mrp_ctx *ctx, void *stream, int M, const float *teacher, const f
 #define MRP_DTYPE_BF16 1
 int mrp_residual_rms(mrp_ctx *ctx, void *stream, int n_blocks, int S, long N, const void *X, int dtype,
                      double *rms_pair, double *rms_delta);
+
+/* ---- Norm and rotation of queries and keys, and a key-value cache in pages ----
+ *
+ * What a decoder layer does around its attention, for the backbone that the chain drafts for and for filling the
+ * prefix caches that mrp_chain_step_tf reads.  Element types:
+ *   MRP_DTYPE_F32, MRP_DTYPE_BF16, MRP_DTYPE_F16, and for caches MRP_DTYPE_E4M3 (8 bits, 4 of exponent, 3 of
+ *   mantissa, largest 448).
+ * Row tensors ([n_rows][heads][head_dim]) have a stride of their own between rows, in elements, so that they may be parts of
+ * a fused projection's output; the heads of a row lie side by side.  Base pointers and row strides are multiples of 16
+ * bytes.  head_dim is 64, 128 or 256; n_heads is a multiple of n_kv_heads and at most 1024; query head x reads key head
+ * x / (n_heads / n_kv_heads).  Outputs must not overlap inputs or each other, unless it says so.  The context gives
+ * messages and the error word only: its sizes do not bound these calls, nothing here uses its workspace, and it has to be of
+ * the current device (MRP_ERR_SHAPE otherwise). */
+#define MRP_DTYPE_F16 2
+#define MRP_DTYPE_E4M3 3
+
+/* out [n_pos][rotary_dim / 2][2] fp32 (16-byte aligned): cos and sin of p * theta^(-2 j / rotary_dim), the angle in 64 bits.
+ * rotary_dim: multiple of 16, 16..256; theta > 1; 1 <= n_pos <= 2^24. */
+int mrp_rope_table(mrp_ctx *ctx, void *stream, int n_pos, int rotary_dim, float theta, float *out);
+
+/* Norm and rotation of the heads of q and k.  For a head x of head_dim entries in a row at position p:
+ *   n = x / sqrt(mean(x^2) + eps) * gain     (n = x where the gain is NULL)
+ *   y_j = n_j cos(p, j) - n_{j+r} sin(p, j),  y_{j+r} = n_{j+r} cos(p, j) + n_j sin(p, j),  j < r = rotary_dim / 2,
+ *   y_j = n_j for j >= rotary_dim
+ * in 32 bits, rounded once.  All heads of q share q_gain, all heads of k k_gain (n_kv_heads may be 0 where k is not
+ * given).  x_dtype: type of the inputs and their gradients; y_dtype: of the outputs and theirs: the same type, or BF16 or
+ * F16 for inputs of F32. */
+typedef struct {
+    int n_heads, n_kv_heads, head_dim;
+    int rotary_dim;              /* multiple of 16 in [0, head_dim]; 0: no rotation */
+    int x_dtype, y_dtype;
+    int gain_dtype;              /* F32, BF16 or F16 */
+    float eps;                   /* >= 0 */
+    const void *q_gain, *k_gain; /* [head_dim] or NULL */
+    const float *rope;           /* [n_pos][rotary_dim / 2][2] (mrp_rope_table); may be NULL when rotary_dim is 0 */
+    int n_pos;
+} mrp_qk;
+
+/* q_out [n_rows][n_heads][head_dim] and k_out [n_rows][n_kv_heads][head_dim], dense, from q and k; pos int32 [n_rows]. */
+int mrp_qk_norm_rope(mrp_ctx *ctx, void *stream, long n_rows, const mrp_qk *qk, const int32_t *pos, const void *q,
+                     long q_stride, const void *k, long k_stride, void *q_out, void *k_out);
+
+/* Its gradient.  q, k, pos as given to mrp_qk_norm_rope; dq_out, dk_out the gradients of its outputs (dense); dq, dk those of its
+ * inputs (strides of their own); dq_gain, dk_gain fp32 [head_dim] sums over rows and heads, added up in a fixed order, each
+ * NULL where not wanted (and NULL where the gain is).  scratch: mrp_qk_norm_rope_grad_scratch_bytes, 16-byte aligned, of the
+ * caller's; it holds nothing between calls, and calls that may overlap in time need one each. */
+size_t mrp_qk_norm_rope_grad_scratch_bytes(long n_rows, const mrp_qk *qk);
+int mrp_qk_norm_rope_grad(mrp_ctx *ctx, void *stream, long n_rows, const mrp_qk *qk, const int32_t *pos, const void *q,
+                          long q_stride, const void *k, long k_stride, const void *dq_out, const void *dk_out, void *dq,
+                          long dq_stride, void *dk, long dk_stride, float *dq_gain, float *dk_gain, void *scratch,
+                          size_t scratch_bytes);
+
+/* New rows of a batch: sequence b has rows cu_rows[b] .. cu_rows[b + 1] - 1 of the row tensors (cu_rows NULL: rows b * max_new
+ * .. (b + 1) * max_new - 1) and kv_len[b] positions, these rows being the last of them.  The i-th of its n rows has position
+ * kv_len[b] - n + i; a row whose position is negative is padding: nothing of it is cached, and its outputs are zero.  Rows
+ * that belong to no sequence are left as they are. */
+typedef struct {
+    int B;                     /* 0..65535 */
+    int max_new;               /* no sequence has more new rows, >= 1 */
+    const int32_t *cu_rows;    /* [B + 1] or NULL */
+    const int32_t *kv_len;     /* [B] */
+} mrp_new_rows;
+
+/* Keys and values in pages of page_size positions: k_pages, v_pages [n_pages][page_size][n_kv_heads][head_dim], position p of
+ * sequence b at place p % page_size of page page_table[b][p / page_size].  Sequences may share pages that they only read.  A
+ * contiguous cache [B][max_prefix][n_kv_heads][head_dim] is B pages of max_prefix positions with page_table[b] = {b}.
+ * E4M3: an entry stands for scale[kv head] (> 0, fp32 [n_kv_heads]; NULL: 1) times what is stored. */
+typedef struct {
+    void *k_pages, *v_pages;
+    int dtype;                 /* BF16, F16 or E4M3 */
+    int n_kv_heads, head_dim;
+    int n_pages, page_size;    /* n_pages * page_size < 2^31 */
+    const int32_t *page_table; /* [B][max_pages] */
+    int max_pages;             /* max_pages * page_size < 2^31 */
+    const float *k_scale, *v_scale;
+} mrp_paged_cache;
+
+/* Appends the keys and values of the batch's new rows: k normalised and rotated (at the row's position) as by mrp_qk_norm_rope, v as
+ * it is, each rounded once to the cache's type (E4M3: divided by the scale first; beyond 448 saturates, NaN stays).  q_out
+ * [n_rows][n_heads][head_dim], dense, of y_dtype: the queries, normalised and rotated (q NULL: none).  k and v of x_dtype; no two
+ * rows may have the same place. */
+int mrp_cache_append(mrp_ctx *ctx, void *stream, long n_rows, const mrp_new_rows *rows, const mrp_qk *qk, const void *q,
+                     long q_stride, const void *k, long k_stride, const void *v, long v_stride,
+                     const mrp_paged_cache *cache, void *q_out);
+
+/* Attention of the batch's new rows over the cache, which holds their own keys and values too (mrp_cache_append first):
+ *   out = softmax(scale q k^T) v over the positions j that the row, at position p, sees:
+ *   j <= p (causal) or j < kv_len[b] (a block whose rows all see each other), and, with a window, j > p - window or
+ *   j < n_sink.  A row that sees nothing (padding, pages that are not there) has out = 0 and lse = -inf.
+ * What lies in places that no row of a sequence sees, or only others than this row, does not reach its output, whatever it
+ * is; a visible value that is not finite makes the outputs that take it not finite.  Scores and sums are kept in 32 bits, the
+ * softmax weights as the two leading terms of dtype for few rows, as one rounded to dtype for many.
+ * q, out: dtype BF16 or F16, the cache's where that is not E4M3; out [n_rows][n_heads][head_dim] dense; lse fp32
+ * [n_rows][n_heads]: log of the sum of exp(scale q k), or NULL.  scratch: mrp_paged_attention_scratch_bytes, 16-byte aligned, of the
+ * caller's; it holds nothing between calls, and calls that may overlap in time (two graphs on two streams) need one each. */
+typedef struct {
+    int n_heads;
+    int dtype;
+    float scale;               /* > 0 */
+    int causal;                /* 0 or 1 */
+    int window;                /* 0: none */
+    int n_sink;                /* first positions that stay visible behind a window */
+} mrp_attn;
+size_t mrp_paged_attention_scratch_bytes(const mrp_ctx *ctx, long n_rows, const mrp_new_rows *rows,
+                                         const mrp_paged_cache *cache, const mrp_attn *attn);
+int mrp_paged_attention(mrp_ctx *ctx, void *stream, long n_rows, const mrp_new_rows *rows, const mrp_paged_cache *cache,
+                        const mrp_attn *attn, const void *q, long q_stride, void *out, float *lse, void *scratch,
+                        size_t scratch_bytes);
 
 /* Timing of the dominant kernel.  With profiling on, every LM-head kernel
  * launched by mrp_chain_step is bracketed by a pair of HIP events on the call's

@@ -13,6 +13,8 @@ EXPORTED_SYMBOLS = [
     "mrp_pack_weight", "mrp_pack_body_weight", "mrp_chain_step", "mrp_remask", "mrp_commit", "mrp_verify_accept", "mrp_verify_accept_joint", "mrp_kl_loss", "mrp_residual_rms", "mrp_tbody_create", "mrp_chain_step_tf",
     "mrp_profile_enable", "mrp_profile_read", "mrp_verify_accept_static", "mrp_verify_accept_static_scratch_bytes",
     "mrp_build_candidates", "mrp_poll_error", "mrp_probe_lm_traffic",
+    "mrp_rope_table", "mrp_qk_norm_rope", "mrp_qk_norm_rope_grad", "mrp_qk_norm_rope_grad_scratch_bytes",
+    "mrp_cache_append", "mrp_paged_attention", "mrp_paged_attention_scratch_bytes",
 ]
 
 MRP_MAX_HEADS = 16
@@ -52,6 +54,27 @@ class _StepIO(C.Structure):
                 ("masked", C.c_void_p), ("cond_tok", C.c_void_p), ("protect_pos", C.c_void_p),
                 ("draft_pos", C.c_void_p), ("draft_tok", C.c_void_p), ("remasked", C.c_void_p),
                 ("x_tok", C.c_void_p)]
+
+
+class _Qk(C.Structure):
+    _fields_ = [("n_heads", C.c_int), ("n_kv_heads", C.c_int), ("head_dim", C.c_int), ("rotary_dim", C.c_int),
+                ("x_dtype", C.c_int), ("y_dtype", C.c_int), ("gain_dtype", C.c_int), ("eps", C.c_float),
+                ("q_gain", C.c_void_p), ("k_gain", C.c_void_p), ("rope", C.c_void_p), ("n_pos", C.c_int)]
+
+
+class _NewRows(C.Structure):
+    _fields_ = [("B", C.c_int), ("max_new", C.c_int), ("cu_rows", C.c_void_p), ("kv_len", C.c_void_p)]
+
+
+class _PagedCache(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("dtype", C.c_int), ("n_kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("n_pages", C.c_int), ("page_size", C.c_int), ("page_table", C.c_void_p),
+                ("max_pages", C.c_int), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
+
+
+class _Attn(C.Structure):
+    _fields_ = [("n_heads", C.c_int), ("dtype", C.c_int), ("scale", C.c_float), ("causal", C.c_int),
+                ("window", C.c_int), ("n_sink", C.c_int)]
 
 
 _lib = None
@@ -105,6 +128,23 @@ def load_library():
                                          C.c_void_p, C.c_int, C.c_int32, C.c_void_p, C.c_void_p]
     lib.mrp_poll_error.argtypes = [C.c_void_p, C.c_void_p]
     lib.mrp_probe_lm_traffic.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_void_p]
+    lib.mrp_rope_table.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_float, C.c_void_p]
+    lib.mrp_qk_norm_rope.argtypes = [C.c_void_p, C.c_void_p, C.c_long, C.POINTER(_Qk), C.c_void_p, C.c_void_p, C.c_long,
+                                     C.c_void_p, C.c_long, C.c_void_p, C.c_void_p]
+    lib.mrp_qk_norm_rope_grad_scratch_bytes.argtypes = [C.c_long, C.POINTER(_Qk)]
+    lib.mrp_qk_norm_rope_grad_scratch_bytes.restype = C.c_size_t
+    lib.mrp_qk_norm_rope_grad.argtypes = [C.c_void_p, C.c_void_p, C.c_long, C.POINTER(_Qk), C.c_void_p, C.c_void_p,
+                                          C.c_long, C.c_void_p, C.c_long, C.c_void_p, C.c_void_p, C.c_void_p, C.c_long,
+                                          C.c_void_p, C.c_long, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t]
+    lib.mrp_cache_append.argtypes = [C.c_void_p, C.c_void_p, C.c_long, C.POINTER(_NewRows), C.POINTER(_Qk), C.c_void_p,
+                                     C.c_long, C.c_void_p, C.c_long, C.c_void_p, C.c_long, C.POINTER(_PagedCache),
+                                     C.c_void_p]
+    lib.mrp_paged_attention_scratch_bytes.argtypes = [C.c_void_p, C.c_long, C.POINTER(_NewRows), C.POINTER(_PagedCache),
+                                                      C.POINTER(_Attn)]
+    lib.mrp_paged_attention_scratch_bytes.restype = C.c_size_t
+    lib.mrp_paged_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_long, C.POINTER(_NewRows), C.POINTER(_PagedCache),
+                                        C.POINTER(_Attn), C.c_void_p, C.c_long, C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_size_t]
     lib.mrp_profile_enable.argtypes = [C.c_void_p, C.c_int]
     lib.mrp_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.c_int]
     _lib = lib
@@ -118,6 +158,44 @@ def _ptr(t) -> Optional[int]:
     if not t.is_cuda or not t.is_contiguous():
         raise MrpError("tensor must be a contiguous device tensor")
     return t.data_ptr()
+
+
+_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2, "torch.float8_e4m3fn": 3}
+
+
+def _dtype(t, allowed: str) -> int:
+    code = _DTYPES.get(str(t.dtype), -1)
+    if code < 0 or str(code) not in allowed:
+        raise MrpError(f"no form for tensors of {t.dtype} here")
+    return code
+
+
+def _plain(t, name: str, dtypes: str, shape) -> Optional[int]:
+    """Address of a dense device tensor of one of the types and of this shape (None stays NULL)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape):
+        raise MrpError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if dtypes == "i":
+        if str(t.dtype) != "torch.int32":
+            raise MrpError(f"{name}: {t.dtype}, expected int32")
+    else:
+        _dtype(t, dtypes)
+    return _ptr(t)
+
+
+def _row_tensor(t, name: str, heads: int, head_dim: int, n_rows: int, dtype: int):
+    """(address, row stride) of a device tensor [n_rows][heads][head_dim] whose rows are dense in themselves."""
+    if t is None:
+        return None, 0
+    if tuple(t.shape) != (n_rows, heads, head_dim):
+        raise MrpError(f"{name}: shape {tuple(t.shape)}, expected {(n_rows, heads, head_dim)}")
+    if _DTYPES.get(str(t.dtype), -1) != dtype:
+        raise MrpError(f"{name}: {t.dtype} is not the type that the others have")
+    st = t.stride()
+    if not t.is_cuda or st[2] != 1 or (heads > 1 and st[1] != head_dim):
+        raise MrpError(f"{name}: a device tensor whose heads lie side by side is needed")
+    return t.data_ptr(), (st[0] if n_rows > 1 else heads * head_dim)
 
 
 def _stream() -> int:
@@ -187,6 +265,69 @@ class RevealCfg:
     remask_mode: int = 0
 
 
+class QkNormRope:
+    """Norm and rotation of the heads of q and k (mrp_qk): gains [head_dim] or None, ``rope`` the table
+    [n_pos][rotary_dim / 2][2] of MrpContext.rope_table or None.  The types of the inputs and outputs come with the
+    tensors of a call.  Keeps the tensors that it is given."""
+
+    def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, rope=None, q_gain=None, k_gain=None,
+                 eps: float = 1e-6):
+        gain = q_gain if q_gain is not None else k_gain
+        if q_gain is not None and k_gain is not None and q_gain.dtype != k_gain.dtype:
+            raise MrpError("gains of two types")
+        rot, n_pos = 0, 0
+        if rope is not None:
+            n_pos, rot = rope.shape[0], 2 * rope.shape[1]
+        self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim = n_heads, n_kv_heads, head_dim, rot
+        self.tensors = (rope, q_gain, k_gain)
+        self.c = _Qk(n_heads, n_kv_heads, head_dim, rot, 0, 0, 1 if gain is None else _dtype(gain, "012"), eps,
+                     _plain(q_gain, "q_gain", "012", (head_dim,)), _plain(k_gain, "k_gain", "012", (head_dim,)),
+                     _plain(rope, "rope", "0", (n_pos, rot // 2, 2)), n_pos)
+
+    def typed(self, x_dtype: int, y_dtype: int) -> _Qk:
+        c = _Qk()
+        C.memmove(C.byref(c), C.byref(self.c), C.sizeof(_Qk))
+        c.x_dtype, c.y_dtype = x_dtype, y_dtype
+        return c
+
+
+class NewRows:
+    """New rows of a batch (mrp_new_rows): ``kv_len`` int32 [B] positions with the new rows, at most ``max_new`` rows a
+    sequence, ``cu_rows`` int32 [B + 1] or None where every sequence has max_new."""
+
+    def __init__(self, kv_len, max_new: int, cu_rows=None):
+        self.B = kv_len.shape[0]
+        self.tensors = (kv_len, cu_rows)
+        self.c = _NewRows(self.B, max_new, _plain(cu_rows, "cu_rows", "i", (self.B + 1,)),
+                          _plain(kv_len, "kv_len", "i", (self.B,)))
+
+
+class PagedCache:
+    """Keys and values in pages (mrp_paged_cache): k_pages, v_pages [n_pages][page_size][n_kv_heads][head_dim] of bf16,
+    fp16 or float8_e4m3fn, page_table int32 [B][max_pages], scales fp32 [n_kv_heads] for 8 bits."""
+
+    def __init__(self, k_pages, v_pages, page_table, k_scale=None, v_scale=None):
+        if k_pages.dim() != 4 or v_pages.dtype != k_pages.dtype or page_table.dim() != 2:
+            raise MrpError("pages [n_pages][page_size][n_kv_heads][head_dim] of one type and a table [B][max_pages] are needed")
+        n, ps, hkv, hd = k_pages.shape
+        self.B, self.n_kv_heads, self.head_dim, self.dtype = page_table.shape[0], hkv, hd, _dtype(k_pages, "123")
+        self.tensors = (k_pages, v_pages, page_table, k_scale, v_scale)
+        self.c = _PagedCache(_ptr(k_pages), _plain(v_pages, "v_pages", "123", k_pages.shape), self.dtype, hkv, hd, n, ps,
+                             _plain(page_table, "page_table", "i", page_table.shape), page_table.shape[1],
+                             _plain(k_scale, "k_scale", "0", (hkv,)), _plain(v_scale, "v_scale", "0", (hkv,)))
+
+
+@dataclass
+class AttnCfg:
+    """Attention over a paged cache (mrp_attn): the rows of a sequence see all its positions (causal False) or those up to
+    their own, with ``window`` > 0 only the last ``window`` of them and the first ``n_sink``."""
+    n_heads: int
+    scale: float
+    causal: bool = True
+    window: int = 0
+    n_sink: int = 0
+
+
 class StepIO:
     """Device buffers of one chain step (allocated with torch)."""
 
@@ -227,6 +368,7 @@ class MrpContext:
         if rc != 0:
             raise MrpError(f"mrp_create failed: {rc}")
         self._h = h
+        self.device = torch.cuda.current_device()
 
     def close(self):
         if getattr(self, "_h", None):
@@ -363,6 +505,101 @@ class MrpContext:
         rc = self.lib.mrp_residual_rms(self._h, _stream(), n_blocks, S, N, _ptr(X), 1 if bf16 else 0,
                                        _ptr(rms_pair), _ptr(rms_delta))
         return self._check(rc, "mrp_residual_rms") if check else rc
+
+    def _here(self, *tensors):
+        """The tensors are on the context's device (the call itself refuses another current device)."""
+        for t in tensors:
+            if t is not None and t.get_device() != self.device:
+                raise MrpError(f"a tensor on {t.device}: the context is of device {self.device}")
+
+    def rope_table(self, n_pos: int, rotary_dim: int, theta: float):
+        """cos and sin of every position and pair: fp32 [n_pos][rotary_dim / 2][2]."""
+        import torch
+        out = torch.empty((n_pos, rotary_dim // 2, 2), dtype=torch.float32, device=f"cuda:{self.device}")
+        self._check(self.lib.mrp_rope_table(self._h, _stream(), n_pos, rotary_dim, theta, _ptr(out)), "mrp_rope_table")
+        return out
+
+    def qk_norm_rope(self, qk: QkNormRope, pos, q, k, q_out, k_out, check: bool = True) -> int:
+        """q [n][n_heads][head_dim], k [n][n_kv_heads][head_dim] -> q_out, k_out; pos int32 [n]."""
+        n = q.shape[0]
+        self._here(pos, q, k, q_out, k_out, *qk.tensors)
+        x, y = _dtype(q, "012"), _dtype(q_out, "012")
+        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
+        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
+        rc = self.lib.mrp_qk_norm_rope(self._h, _stream(), n, C.byref(qk.typed(x, y)), _plain(pos, "pos", "i", (n,)), qp, qs,
+                                       kp, ks, _plain(q_out, "q_out", str(y), (n, qk.n_heads, qk.head_dim)),
+                                       _plain(k_out, "k_out", str(y), (n, qk.n_kv_heads, qk.head_dim)))
+        return self._check(rc, "mrp_qk_norm_rope") if check else rc
+
+    def qk_norm_rope_grad(self, qk: QkNormRope, pos, q, k, dq_out, dk_out, dq, dk, dq_gain=None, dk_gain=None, scratch=None,
+                          check: bool = True) -> int:
+        """Gradients of qk_norm_rope: dq, dk (like q, k) and the gains' (fp32 [head_dim]) from dq_out, dk_out.  scratch: a
+        uint8 tensor of qk_norm_rope_grad_scratch_bytes, or None to take one from torch's allocator."""
+        import torch
+        n = q.shape[0]
+        self._here(pos, q, k, dq_out, dk_out, dq, dk, dq_gain, dk_gain, scratch, *qk.tensors)
+        x, y = _dtype(q, "012"), _dtype(dq_out, "012")
+        c = qk.typed(x, y)
+        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
+        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
+        dqp, dqs = _row_tensor(dq, "dq", qk.n_heads, qk.head_dim, n, x)
+        dkp, dks = _row_tensor(dk, "dk", qk.n_kv_heads, qk.head_dim, n, x)
+        if scratch is None:
+            scratch = torch.empty(self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, C.byref(c)), dtype=torch.uint8, device=q.device)
+        rc = self.lib.mrp_qk_norm_rope_grad(self._h, _stream(), n, C.byref(c), _plain(pos, "pos", "i", (n,)), qp, qs, kp, ks,
+                                            _plain(dq_out, "dq_out", str(y), (n, qk.n_heads, qk.head_dim)),
+                                            _plain(dk_out, "dk_out", str(y), (n, qk.n_kv_heads, qk.head_dim)), dqp, dqs, dkp, dks,
+                                            _plain(dq_gain, "dq_gain", "0", (qk.head_dim,)),
+                                            _plain(dk_gain, "dk_gain", "0", (qk.head_dim,)), _ptr(scratch),
+                                            scratch.numel() * scratch.element_size())
+        return self._check(rc, "mrp_qk_norm_rope_grad") if check else rc
+
+    def qk_norm_rope_grad_scratch_bytes(self, qk: QkNormRope, n: int) -> int:
+        return self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, C.byref(qk.c))
+
+    def cache_append(self, rows: NewRows, qk: QkNormRope, q, k, v, cache: PagedCache, q_out, check: bool = True) -> int:
+        """Norm, rotate and append k, append v, and norm and rotate q into q_out (q and q_out None: keys and values only)."""
+        n = k.shape[0]
+        self._here(q, k, v, q_out, *rows.tensors, *qk.tensors, *cache.tensors)
+        if rows.B != cache.B:
+            raise MrpError(f"{rows.B} sequences, but a page table of {cache.B}")
+        if (q is None) != (q_out is None):
+            raise MrpError("q and q_out go together")
+        x = _dtype(k, "012")
+        y = x if q_out is None else _dtype(q_out, "012")
+        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
+        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
+        vp, vs = _row_tensor(v, "v", qk.n_kv_heads, qk.head_dim, n, x)
+        rc = self.lib.mrp_cache_append(self._h, _stream(), n, C.byref(rows.c), C.byref(qk.typed(x, y)), qp, qs, kp, ks, vp, vs,
+                                       C.byref(cache.c), _plain(q_out, "q_out", str(y), (n, qk.n_heads, qk.head_dim)))
+        return self._check(rc, "mrp_cache_append") if check else rc
+
+    def _attn(self, cfg: AttnCfg, q) -> _Attn:
+        return _Attn(cfg.n_heads, _dtype(q, "12"), cfg.scale, 1 if cfg.causal else 0, cfg.window, cfg.n_sink)
+
+    def paged_attention_scratch_bytes(self, rows: NewRows, cache: PagedCache, cfg: AttnCfg, q) -> int:
+        return self.lib.mrp_paged_attention_scratch_bytes(self._h, q.shape[0], C.byref(rows.c), C.byref(cache.c),
+                                                          C.byref(self._attn(cfg, q)))
+
+    def paged_attention(self, rows: NewRows, cache: PagedCache, cfg: AttnCfg, q, out, lse=None, scratch=None,
+                        check: bool = True) -> int:
+        """out [n][n_heads][head_dim] (lse fp32 [n][n_heads], or None) of q over the cache.  scratch: a uint8 tensor of
+        paged_attention_scratch_bytes, or None to take one from torch's allocator."""
+        import torch
+        n = q.shape[0]
+        self._here(q, out, lse, scratch, *rows.tensors, *cache.tensors)
+        if rows.B != cache.B:
+            raise MrpError(f"{rows.B} sequences, but a page table of {cache.B}")
+        a = self._attn(cfg, q)
+        qp, qs = _row_tensor(q, "q", cfg.n_heads, cache.head_dim, n, a.dtype)
+        if scratch is None:
+            need = self.lib.mrp_paged_attention_scratch_bytes(self._h, n, C.byref(rows.c), C.byref(cache.c), C.byref(a))
+            scratch = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        rc = self.lib.mrp_paged_attention(self._h, _stream(), n, C.byref(rows.c), C.byref(cache.c), C.byref(a), qp, qs,
+                                          _plain(out, "out", str(a.dtype), (n, cfg.n_heads, cache.head_dim)),
+                                          _plain(lse, "lse", "0", (n, cfg.n_heads)), _ptr(scratch),
+                                          0 if scratch is None else scratch.numel() * scratch.element_size())
+        return self._check(rc, "mrp_paged_attention") if check else rc
 
     def profile_enable(self, on: bool):
         self._check(self.lib.mrp_profile_enable(self._h, 1 if on else 0), "mrp_profile_enable")

@@ -140,6 +140,16 @@ bool small_rows_kernel(int M, int Kc) { return !body_on_tiles(M, Kc); }
 
 }  // namespace
 
+CtxView mrp::ctx_view(const mrp_ctx *c) { return CtxView{c->device, c->nCU, c->err_flag}; }
+
+int mrp::ctx_fail(mrp_ctx *c, int code, const char *fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(c->err, sizeof(c->err), fmt, ap);
+    va_end(ap);
+    return code;
+}
+
 // LM head of M rows on the tile kernel?  The persistent kernel streams W_lm once through all CUs and is bound by that
 // stream up to 128 rows; its 256-row form pays for 256 rows whatever M is, and rows beyond stream W_lm a second time.
 // The tile kernel pays for the 32-row blocks it needs, in whole rounds of one tile per CU.  Measured (us, persistent / tile
@@ -926,11 +936,15 @@ int mrp_poll_error(mrp_ctx *c, void *stream) {
     HIP_TRY(c, hipMemcpy(&flags, c->err_flag, sizeof(int), hipMemcpyDeviceToHost));
     if (flags) {
         HIP_TRY(c, hipMemset(c->err_flag, 0, sizeof(int)));
-        snprintf(c->err, sizeof(c->err), "device error word 0x%x:%s%s%s%s", (unsigned)flags,
+        snprintf(c->err, sizeof(c->err), "device error word 0x%x:%s%s%s%s%s%s%s%s", (unsigned)flags,
                  (flags & MRP_FLAG_COND_TOK) ? " cond_tok out of range (clamped)" : "",
                  (flags & MRP_FLAG_DRAFT_POS) ? " draft position >= block length (taken as missing)" : "",
                  (flags & MRP_FLAG_PREFIX_LEN) ? " prefix_len outside [0, max_prefix] (clamped)" : "",
-                 (flags & MRP_FLAG_X_TOK) ? " recorded token >= V (clamped)" : "");
+                 (flags & MRP_FLAG_X_TOK) ? " recorded token >= V (clamped)" : "",
+                 (flags & MRP_FLAG_POSITION) ? " position outside the rotation table (clamped)" : "",
+                 (flags & MRP_FLAG_ROWS) ? " cu_rows out of range (clamped)" : "",
+                 (flags & MRP_FLAG_KV_LEN) ? " kv_len outside the page table (clamped)" : "",
+                 (flags & MRP_FLAG_PAGE) ? " page number outside [0, n_pages) (skipped)" : "");
     }
     return flags;
 }

@@ -4,7 +4,17 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+struct mrp_ctx;
+
 namespace mrp {
+
+// What the entry points outside mrp_api.hip use of a context
+struct CtxView {
+    int device, nCU;
+    int *err_flag;
+};
+CtxView ctx_view(const mrp_ctx *c);
+int ctx_fail(mrp_ctx *c, int code, const char *fmt, ...);   // sets the message, returns the code
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -87,7 +97,7 @@ struct TiledGemmArgs {
 
 // Bits of a context's device error word (the MRP_FLAG_* values of include/mrp.h): an index the caller
 // passed in device memory was out of range; the kernel clamped or skipped it and reports it here.
-enum { ERR_COND_TOK = 1, ERR_DRAFT_POS = 2, ERR_PREFIX_LEN = 4, ERR_X_TOK = 8 };
+enum { ERR_COND_TOK = 1, ERR_DRAFT_POS = 2, ERR_PREFIX_LEN = 4, ERR_X_TOK = 8, ERR_POSITION = 16, ERR_ROWS = 32, ERR_KV_LEN = 64, ERR_PAGE = 128 };
 
 // MLP head body for fewer than 768 activation rows without partial sums in memory (head_fused.hip)
 struct HeadFusedArgs {

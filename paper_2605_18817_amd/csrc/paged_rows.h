@@ -1,0 +1,89 @@
+// Element types and the rows of a ragged batch, as the kernels around a paged cache read them.
+#pragma once
+#include "../../include/mrp.h"
+#include "mrp_kernels.h"
+
+namespace mrp {
+
+struct F32 {};
+struct BF16 {};
+struct F16 {};
+
+__device__ __forceinline__ void load8(const void *base, long at, F32, float (&x)[8]) {
+    const float4 *p = reinterpret_cast<const float4 *>(static_cast<const float *>(base) + at);
+    const float4 a = p[0], b = p[1];
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void load8(const void *base, long at, BF16, float (&x)[8]) {
+    unpack_bf16x8(*reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(base) + at), x);
+}
+__device__ __forceinline__ void load8(const void *base, long at, F16, float (&x)[8]) {
+    const f16x8 v = *reinterpret_cast<const f16x8 *>(static_cast<const uint16_t *>(base) + at);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
+}
+__device__ __forceinline__ void store8(void *base, long at, F32, const float (&x)[8]) {
+    float4 *p = reinterpret_cast<float4 *>(static_cast<float *>(base) + at);
+    p[0] = make_float4(x[0], x[1], x[2], x[3]);
+    p[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(void *base, long at, BF16, const float (&x)[8]) {
+    bf16x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (__bf16)x[e];
+    *reinterpret_cast<bf16x8 *>(static_cast<uint16_t *>(base) + at) = v;
+}
+__device__ __forceinline__ void store8(void *base, long at, F16, const float (&x)[8]) {
+    f16x8 v;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (_Float16)x[e];
+    *reinterpret_cast<f16x8 *>(static_cast<uint16_t *>(base) + at) = v;
+}
+// Round to nearest, ties to even; beyond 448 saturates, NaN stays
+__device__ __forceinline__ float e4m3_range(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
+__device__ __forceinline__ void store8_e4m3(void *base, long at, const float (&x)[8]) {
+    int lo = 0, hi = 0;
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[0]), e4m3_range(x[1]), lo, false);
+    lo = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[2]), e4m3_range(x[3]), lo, true);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[4]), e4m3_range(x[5]), hi, false);
+    hi = __builtin_amdgcn_cvt_pk_fp8_f32(e4m3_range(x[6]), e4m3_range(x[7]), hi, true);
+    *reinterpret_cast<int2 *>(static_cast<uint8_t *>(base) + at) = make_int2(lo, hi);
+}
+
+// The new rows of one sequence, out of range values clamped
+struct SeqRows {
+    int begin, n;   // its first row, and how many
+    int len;        // positions, the new rows included
+};
+__device__ __forceinline__ SeqRows seq_rows(const mrp_new_rows &r, int n_rows, long cap, int b) {
+    SeqRows s;
+    if (r.cu_rows) {
+        const int a = r.cu_rows[b], e = r.cu_rows[b + 1];
+        s.begin = a < 0 ? 0 : (a > n_rows ? n_rows : a);
+        const int end = e > n_rows ? n_rows : e;
+        s.n = end < s.begin ? 0 : end - s.begin;
+    } else {
+        s.begin = b * r.max_new;
+        s.n = r.max_new;
+    }
+    if (s.n > r.max_new) s.n = r.max_new;
+    const int len = r.kv_len[b];
+    s.len = len < 0 ? 0 : (len > cap ? (int)cap : len);
+    return s;
+}
+// Reports what seq_rows clamps; called by one workgroup of `threads` threads
+__device__ __forceinline__ void check_rows(const mrp_new_rows &r, int n_rows, long cap, int *err_flag, int threads) {
+    int bad = 0;
+    for (int b = threadIdx.x; b < r.B; b += threads) {
+        if (r.cu_rows) {
+            const int a = r.cu_rows[b], e = r.cu_rows[b + 1];
+            if (a < 0 || e < a || e > n_rows || e - a > r.max_new) bad |= ERR_ROWS;
+        }
+        const int len = r.kv_len[b];
+        if (len < 0 || len > cap) bad |= ERR_KV_LEN;
+    }
+    if (bad) atomicOr(err_flag, bad);
+}
+
+}  // namespace mrp
