@@ -1,0 +1,141 @@
+// What the two forms of the attention over a paged cache share: element types, which positions a row sees, and how a row is stored.
+#pragma once
+#include "paged_rows.h"
+
+namespace mrp {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma(BF16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma(F16, u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// two values rounded to nearest, and what the rounding left
+__device__ __forceinline__ uint32_t pack2(BF16, float x, float y, float &rx, float &ry) {
+    const bf16x2 h = {(__bf16)x, (__bf16)y};
+    rx = x - (float)h[0];
+    ry = y - (float)h[1];
+    return __builtin_bit_cast(uint32_t, h);
+}
+__device__ __forceinline__ uint32_t pack2(F16, float x, float y, float &rx, float &ry) {
+    const f16x2 h = {(_Float16)x, (_Float16)y};
+    rx = x - (float)h[0];
+    ry = y - (float)h[1];
+    return __builtin_bit_cast(uint32_t, h);
+}
+// four e4m3 values as 16-bit ones (exact in both types)
+__device__ __forceinline__ void widen(BF16, uint32_t v, uint32_t &lo, uint32_t &hi) {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, true));
+}
+__device__ __forceinline__ void widen(F16, uint32_t v, uint32_t &lo, uint32_t &hi) {
+    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, false));
+    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, true));
+}
+template <typename T>
+__device__ __forceinline__ bool not_finite(T, uint32_t v) {   // either half
+    constexpr uint32_t E = __is_same(T, BF16) ? 0x7f80u : 0x7c00u;
+    return (v & E) == E || ((v >> 16) & E) == E;
+}
+
+__device__ __forceinline__ float to_float(BF16, uint32_t half) { return __uint_as_float(half << 16); }
+__device__ __forceinline__ float to_float(F16, uint32_t half) { return (float)__builtin_bit_cast(_Float16, (uint16_t)half); }
+template <typename T>
+__device__ __forceinline__ uint32_t finite_halves(T, uint32_t v) {   // halves that are not finite cleared
+    constexpr uint32_t E = __is_same(T, BF16) ? 0x7f80u : 0x7c00u;
+    if ((v & E) == E) v &= 0xffff0000u;
+    if (((v >> 16) & E) == E) v &= 0xffffu;
+    return v;
+}
+
+struct Attend {
+    mrp_new_rows rows;
+    mrp_paged_cache cache;
+    mrp_attn attn;
+    int n_rows, G;
+    const uint16_t *q;
+    long q_stride;
+    uint16_t *out;
+    float *lse;
+    int *err_flag;
+};
+
+// bits 0 .. n - 1 of 32
+__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
+// which of the positions key0 .. key0 + 31 the row at position p sees
+__device__ __forceinline__ uint32_t seen_bits(int p, int key0, int len, const mrp_attn &a) {
+    const int high = p < 0 ? 0 : (a.causal ? p + 1 : len);
+    uint32_t seen = first_bits(high - key0);
+    if (a.window) seen &= ~first_bits(p + 1 - a.window - key0) | first_bits(a.n_sink - key0);
+    return seen;
+}
+
+// N dwords of a lane's share
+template <int N>
+struct Words {
+    uint32_t w[N];
+};
+template <int N>
+__device__ __forceinline__ Words<N> load_words(const char *p) {
+    Words<N> r;
+    if constexpr (N >= 4) {
+#pragma unroll
+        for (int i = 0; i < N / 4; ++i) {
+            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
+            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+        }
+    } else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(p);
+        r.w[0] = v.x; r.w[1] = v.y;
+    } else {
+        r.w[0] = *reinterpret_cast<const uint32_t *>(p);
+    }
+    return r;
+}
+
+// A row's part: normalised, rounded, and its log-sum (m2: the reference in units of log 2)
+template <typename T, int HD>
+__device__ __forceinline__ void store_row(const Attend &A, long row, int head, int part, bool empty, float m2, float sum, float v_scale,
+                                          float (&o)[HD / 16]) {
+    constexpr int NE = HD / 16;
+    const float f = v_scale / sum;
+    uint32_t *dst = reinterpret_cast<uint32_t *>(A.out + (row * A.attn.n_heads + head) * HD + NE * part);
+    float x, y;
+    Words<NE / 2> w;
+#pragma unroll
+    for (int e = 0; e < NE; e += 2) w.w[e / 2] = empty ? 0u : pack2(T{}, o[e] * f, o[e + 1] * f, x, y);
+#pragma unroll
+    for (int e = 0; e < NE / 2; ++e) dst[e] = w.w[e];
+    if (A.lse && part == 0) A.lse[row * A.attn.n_heads + head] = empty ? -INFINITY : m2 * 0.6931471805599453f + logf(sum);
+}
+
+// Steps of STEP positions for rows at p_first .. p_last of a sequence: [0, sink) in s_steps of them, [low, high) from step `first`
+struct Steps {
+    int first, s_steps, steps, low, high;
+};
+template <int STEP>
+__device__ __forceinline__ Steps steps_of(const mrp_attn &a, int p_first, int p_last, int len) {
+    Steps t;
+    t.high = p_last < 0 ? 0 : (a.causal ? p_last + 1 : len);
+    t.low = a.window && p_first + 1 > a.window ? p_first + 1 - a.window : 0;
+    t.first = t.low / STEP;
+    const int want = ((a.n_sink < t.low ? a.n_sink : t.low) + STEP - 1) / STEP;
+    t.s_steps = want < t.first ? want : t.first;
+    t.steps = t.high > 0 ? t.s_steps + (t.high + STEP - 1) / STEP - t.first : 0;
+    return t;
+}
+
+// Most rows of a key head that a sequence can have
+inline long most_rows(long n_rows, const mrp_new_rows &r, int G) { return (long)G * (r.max_new < n_rows ? r.max_new : n_rows); }
+
+// Attention of many rows (prompt_attention.hip): does it take this call, its scratch, and its launch
+bool prompt_takes(long rows, int head_dim);
+size_t prompt_scratch_floats(long rows, int B, int n_kv_heads, long positions, int head_dim, int nCU);
+hipError_t launch_prompt_attention(const Attend &a, float *scratch, int nCU, hipStream_t st);
+
+}  // namespace mrp

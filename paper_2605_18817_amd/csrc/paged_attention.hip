@@ -13,7 +13,7 @@
 // 8 (m / 4) + 4 t + m % 4), and the weights never leave their lane.  V^T is built in registers: a lane loads its 16th of the
 // entries of 8 positions and exchanges 16-bit halves between them; entry e of every lane's share makes up one A operand.  Nothing
 // goes through shared memory until the waves of a workgroup, which take the steps of a sequence in turn, add up.
-#include "paged_rows.h"
+#include "paged_attention.h"
 
 namespace mrp {
 
@@ -23,393 +23,521 @@ int check_context_device(mrp_ctx *c, const char *what);
 
 namespace {
 
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
 constexpr int WAVES = 4;
 constexpr int STEP = 32;     // positions per step of a wave
 
-__device__ __forceinline__ f32x4 mfma(BF16, u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma(F16, u32x4 a, u32x4 b, f32x4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-// two values rounded to nearest, and what the rounding left
-__device__ __forceinline__ uint32_t pack2(BF16, float x, float y, float &rx, float &ry) {
-    const bf16x2 h = {(__bf16)x, (__bf16)y};
-    rx = x - (float)h[0];
-    ry = y - (float)h[1];
-    return __builtin_bit_cast(uint32_t, h);
-}
-__device__ __forceinline__ uint32_t pack2(F16, float x, float y, float &rx, float &ry) {
-    const f16x2 h = {(_Float16)x, (_Float16)y};
-    rx = x - (float)h[0];
-    ry = y - (float)h[1];
-    return __builtin_bit_cast(uint32_t, h);
-}
-// four e4m3 values as 16-bit ones (exact in both types)
-__device__ __forceinline__ void widen(BF16, uint32_t v, uint32_t &lo, uint32_t &hi) {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, true));
-}
-__device__ __forceinline__ void widen(F16, uint32_t v, uint32_t &lo, uint32_t &hi) {
-    lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, false));
-    hi = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.0f, true));
-}
-template <typename T>
-__device__ __forceinline__ bool not_finite(T, uint32_t v) {   // either half
-    constexpr uint32_t E = sizeof(T) && __is_same(T, BF16) ? 0x7f80u : 0x7c00u;
-    return (v & E) == E || ((v >> 16) & E) == E;
-}
-
-struct Attend {
-    mrp_new_rows rows;
-    mrp_paged_cache cache;
-    mrp_attn attn;
-    int n_rows, G;
-    const uint16_t *q;
-    long q_stride;
-    uint16_t *out;
-    float *lse;
-    int *err_flag;
+// ---- how the work is split
+//
+// A sequence's steps come in units of WAVES, and units(b) counts those that any of its rows needs.  Its items, one for each key
+// head and tile of 16 RT rows, take that many units each, and the units of all items of all sequences, in order, are cut
+// into as many equal ranges as there are workgroups.  A range that ends inside an item leaves a partial result (sums, their reference m, and
+// l) in one of the workgroup's two places: place 1 if it has the item's first unit, place 0 otherwise; an item's pieces are then
+// added up in order by a second kernel.  Every kernel works the cut out anew from the lengths: nothing is planned on the host,
+// which does not know them.
+struct Split {
+    int rows;          // rows of a tile
+    int min_units;     // a workgroup takes at least so many
+    int workgroups;    // at most
 };
 
-// bits 0 .. n - 1 of 32
-__device__ __forceinline__ uint32_t first_bits(int n) { return n <= 0 ? 0u : (n >= 32 ? 0xffffffffu : (1u << n) - 1u); }
-// which of the positions key0 .. key0 + 31 the row at position p sees
-__device__ __forceinline__ uint32_t seen_bits(int p, int key0, int len, const mrp_attn &a) {
-    const int high = p < 0 ? 0 : (a.causal ? p + 1 : len);
-    uint32_t seen = first_bits(high - key0);
-    if (a.window) seen &= ~first_bits(p + 1 - a.window - key0) | first_bits(a.n_sink - key0);
-    return seen;
+__device__ __forceinline__ int units_of(const Attend &A, const SeqRows &s) {
+    const int u = (steps_of<STEP>(A.attn, s.len - s.n, s.len - 1, s.len).steps + WAVES - 1) / WAVES;
+    return u > 1 ? u : 1;
 }
-
-// N dwords of a lane's share
-template <int N>
-struct Words {
-    uint32_t w[N];
-};
-template <int N>
-__device__ __forceinline__ Words<N> load_words(const char *p) {
-    Words<N> r;
-    if constexpr (N >= 4) {
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) {
-            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
-        }
-    } else if constexpr (N == 2) {
-        const uint2 v = *reinterpret_cast<const uint2 *>(p);
-        r.w[0] = v.x; r.w[1] = v.y;
-    } else {
-        r.w[0] = *reinterpret_cast<const uint32_t *>(p);
-    }
-    return r;
+__device__ __forceinline__ long cost_of(const Attend &A, const Split &P, const SeqRows &s) {
+    return s.n ? (long)A.cache.n_kv_heads * ((s.n * A.G + P.rows - 1) / P.rows) * units_of(A, s) : 0;
 }
+__device__ __forceinline__ long block_sum(long x, long *tmp) {   // over 256 threads
+    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = x;
+    __syncthreads();
+    return (tmp[0] + tmp[1]) + (tmp[2] + tmp[3]);
+}
+__device__ __forceinline__ int ranges(const Split &P, long total) {
+    const long most = total / P.min_units;
+    return most < 1 ? 1 : (most < P.workgroups ? (int)most : P.workgroups);
+}
+__device__ __forceinline__ long range_begin(long total, int n, int w) { return total / n * w + total % n * w / n; }
 
-template <typename T, bool E8, int HD, int RT>
-__global__ __launch_bounds__(64 * WAVES) void paged_attention_kernel(const Attend A) {
+// partial results: per workgroup and place `rows` x (HD sums), then `rows` x (m, l)
+__host__ __device__ constexpr size_t place_floats(int rows, int HD) { return (size_t)rows * (HD + 2); }
+
+template <typename T, bool E8, int HD, int RT, bool AHEAD>
+__global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void paged_attention_kernel(const Attend A, const Split P, float *scratch) {
     constexpr int ES = E8 ? 1 : 2;             // bytes of a cache entry
     constexpr int NC = HD / 32;                // contraction steps of a score
     constexpr int NE = HD / 16;                // entries of a lane's share of V, and A operands of O^T
+    constexpr int NL = E8 ? NC / 2 : NC;       // 16-byte pieces of a lane's share of K
     __shared__ float sm[WAVES][16 * RT], sl[WAVES][16 * RT];
-    __shared__ float so[WAVES][16][HD + 4];
+    __shared__ __align__(16) float so[WAVES][16][HD + 4];
+    __shared__ uint16_t sw[WAVES][32 * 16 * RT];
+    __shared__ long scan[WAVES];
+    __shared__ long seq_base;
+    __shared__ int seq_at;
 
     const mrp_paged_cache &C = A.cache;
     const long cap = (long)C.max_pages * C.page_size;
-    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0) check_rows(A.rows, A.n_rows, cap, A.err_flag, 64 * WAVES);
-    const int b = blockIdx.z, kvh = blockIdx.y, G = A.G;
-    const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
-    const int row0 = blockIdx.x * 16 * RT, nr = s.n * G;
-    if (row0 >= nr) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4;
+    if (blockIdx.x == 0) check_rows(A.rows, A.n_rows, cap, A.err_flag, 64 * WAVES);
 
-    // the rows' positions and operands; lanes past the last row take it again and store nothing
-    int pos[RT];
-    u32x4 qf[RT][NC];
-    const int t_first = row0 / G, t_last = (row0 + 16 * RT < nr ? row0 + 16 * RT - 1 : nr - 1) / G;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        const int r = row0 + 16 * rt + r16 < nr ? row0 + 16 * rt + r16 : nr - 1;
-        const int t = r / G;
-        pos[rt] = s.len - s.n + t;
-        const uint16_t *qp = A.q + (long)(s.begin + t) * A.q_stride + (long)(kvh * G + r - t * G) * HD;
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            // (8 bits: a lane's 16 bytes are 16 entries, for two contraction steps)
-            const int at = E8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
-            qf[rt][c] = *reinterpret_cast<const u32x4 *>(qp + at);
+    // this workgroup's range, and the sequence that it begins in
+    long cur, end, base;
+    int b;
+    {
+        const int per = (A.rows.B + 64 * WAVES - 1) / (64 * WAVES), b0 = threadIdx.x * per;
+        long mine = 0;
+        for (int i = b0; i < b0 + per && i < A.rows.B; ++i) mine += cost_of(A, P, seq_rows(A.rows, A.n_rows, cap, i));
+        long incl = mine;
+        for (int off = 1; off < 64; off <<= 1) {
+            const long y = __shfl_up(incl, off);
+            if ((threadIdx.x & 63) >= off) incl += y;
         }
+        if ((threadIdx.x & 63) == 63) scan[threadIdx.x >> 6] = incl;
+        __syncthreads();
+        long before = 0, total = 0;
+        for (int w = 0; w < WAVES; ++w) {
+            if (w < (int)(threadIdx.x >> 6)) before += scan[w];
+            total += scan[w];
+        }
+        const int n = ranges(P, total);
+        if ((int)blockIdx.x >= n) return;
+        cur = range_begin(total, n, blockIdx.x);
+        end = range_begin(total, n, blockIdx.x + 1);
+        if (cur >= end) return;
+        long at = before + incl - mine;
+        if (at <= cur && cur < at + mine) {
+            int i = b0;
+            for (;; ++i) {
+                const long c = cost_of(A, P, seq_rows(A.rows, A.n_rows, cap, i));
+                if (cur < at + c) break;
+                at += c;
+            }
+            seq_at = i;
+            seq_base = at;
+        }
+        __syncthreads();
+        b = seq_at;
+        base = seq_base;
     }
 
-    // positions that any row sees: [0, sink) and [low, high); [full_low, full_high) is what all rows see
-    const int p_first = s.len - s.n + t_first, p_last = s.len - s.n + t_last, W = A.attn.window;
-    const bool causal = A.attn.causal != 0;
-    const int high = p_last < 0 ? 0 : (causal ? p_last + 1 : s.len);
-    const int full_high = p_first < 0 ? 0 : (causal ? p_first + 1 : s.len);
-    const int low = W && p_first + 1 > W ? p_first + 1 - W : 0;
-    const int full_low = W && p_last + 1 > W ? p_last + 1 - W : 0;
-    const int sink = A.attn.n_sink;
-    const int first = low / STEP;
-    const int s_want = ((sink < low ? sink : low) + STEP - 1) / STEP, s_steps = s_want < first ? s_want : first;
-    const int steps = high > 0 ? s_steps + (high + STEP - 1) / STEP - first : 0;
-
-    const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4, G = A.G;
     const long pitch = (long)C.n_kv_heads * HD * ES;      // bytes between positions
-    const char *kb = static_cast<const char *>(C.k_pages) + (long)kvh * HD * ES;
-    const char *vb = static_cast<const char *>(C.v_pages) + (long)kvh * HD * ES;
-    const int32_t *table = A.cache.page_table + (size_t)b * C.max_pages;
     const bool whole = C.page_size % STEP == 0;           // a step lies in one page
+    const bool causal = A.attn.causal != 0;
+    const int W = A.attn.window, sink = A.attn.n_sink;
 
-    float m[RT], l[RT];
-    f32x4 acc[RT][NE];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
-        l[rt] = 0.f;
-#pragma unroll
-        for (int e = 0; e < NE; ++e) acc[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+    for (;; ++b) {                                        // sequences
+        const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
+        const long cost = cost_of(A, P, s);
+        if (cost == 0) continue;
+        const int units = units_of(A, s), nr = s.n * G, tiles = (nr + P.rows - 1) / P.rows;
+        const int32_t *table = C.page_table + (size_t)b * C.max_pages;
+        while (cur < base + cost && cur < end) {          // items
+            const long item = (cur - base) / units;
+            const int unit0 = (int)(cur - base - item * units), unit1 = units - unit0 <= end - cur ? units : unit0 + (int)(end - cur);
+            const int kvh = (int)(item / tiles), row0 = (int)(item % tiles) * P.rows;
+            cur += unit1 - unit0;
+            __syncthreads();                               // (the item before has been read out of shared memory)
 
-    for (int u = wave; u < steps; u += WAVES) {
-        const int key0 = (u < s_steps ? u : first + u - s_steps) * STEP;
-        // places of the step's positions: one page's, or looked up by lane (key0 + lane % 32)
-        int slot;
-        uint32_t there = 0xffffffffu;                     // positions whose page is there
-        if (whole) {
-            const int page = table[key0 / C.page_size];
-            if (page < 0 || page >= C.n_pages) {
-                if (lane == 0) atomicOr(A.err_flag, ERR_PAGE);
-                continue;
-            }
-            slot = page * C.page_size + key0 % C.page_size + (lane & 31);
-        } else {
-            const int j = key0 + (lane & 31);
-            bool ok = false;
-            slot = 0;
-            if (j < high) {
-                const int page = table[j / C.page_size];
-                ok = page >= 0 && page < C.n_pages;
-                if (ok) slot = page * C.page_size + j % C.page_size;
-                else atomicOr(A.err_flag, ERR_PAGE);
-            }
-            there = (uint32_t)__ballot(ok);
-        }
-        const bool partial = there != 0xffffffffu || key0 + STEP > full_high || (key0 < full_low && key0 + STEP > sink);
-
-        f32x4 sc[RT][2];
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            const char *kp = kb + __shfl(slot, 8 * (r16 >> 2) + 4 * t + (r16 & 3)) * pitch + 16 * g;
-            u32x4 kf[NC];
-            if constexpr (E8) {
-#pragma unroll
-                for (int c = 0; c < NC / 2; ++c) {
-                    const uint4 v = *reinterpret_cast<const uint4 *>(kp + 64 * c);
-                    uint32_t a0, a1, a2, a3;
-                    widen(T{}, v.x, a0, a1);
-                    widen(T{}, v.y, a2, a3);
-                    kf[2 * c] = u32x4{a0, a1, a2, a3};
-                    widen(T{}, v.z, a0, a1);
-                    widen(T{}, v.w, a2, a3);
-                    kf[2 * c + 1] = u32x4{a0, a1, a2, a3};
-                }
-            } else {
-#pragma unroll
-                for (int c = 0; c < NC; ++c) kf[c] = *reinterpret_cast<const u32x4 *>(kp + 64 * c);
-            }
+            // the rows' positions and operands; lanes past the last row take it again and store nothing
+            int pos[RT];
+            u32x4 qf[RT][NC];
+            const int t_first = row0 / G, t_last = (row0 + 16 * RT < nr ? row0 + 16 * RT - 1 : nr - 1) / G;
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                sc[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const int r = row0 + 16 * rt + r16 < nr ? row0 + 16 * rt + r16 : nr - 1;
+                const int t = r / G;
+                pos[rt] = s.len - s.n + t;
+                const uint16_t *qp = A.q + (long)(s.begin + t) * A.q_stride + (long)(kvh * G + r - t * G) * HD;
 #pragma unroll
-                for (int c = 0; c < NC; ++c) sc[rt][t] = mfma(T{}, kf[c], qf[rt][c], sc[rt][t]);
+                for (int c = 0; c < NC; ++c) {
+                    // (8 bits: a lane's 16 bytes are 16 entries, for two contraction steps)
+                    const int at = E8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
+                    qf[rt][c] = *reinterpret_cast<const u32x4 *>(qp + at);
+                }
             }
-        }
-        // the lane's share of V: entries NE r16 .. of positions key0 + 8 g .. + 7
-        Words<NE * ES / 4> vr[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            vr[j] = load_words<NE * ES / 4>(vb + __shfl(slot, 8 * g + j) * pitch + NE * ES * r16);
-        uint32_t vw[8][NE / 2];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            if constexpr (E8) {
-#pragma unroll
-                for (int w = 0; w < NE / 4; ++w) widen(T{}, vr[j].w[w], vw[j][2 * w], vw[j][2 * w + 1]);
-            } else {
-#pragma unroll
-                for (int w = 0; w < NE / 2; ++w) vw[j][w] = vr[j].w[w];
-            }
-        }
 
-        bool odd = false;      // values that are not finite where only some rows see them
-        if (partial) {
-            // scores of positions that a row does not see are dropped, values that no row sees are cleared
+            // positions that any row sees: [0, sink) and [low, high); [full_low, full_high) is what all rows see
+            const int p_first = s.len - s.n + t_first, p_last = s.len - s.n + t_last;
+            const Steps st = steps_of<STEP>(A.attn, p_first, p_last, s.len);
+            const int low = st.low, high = st.high;
+            const int full_high = p_first < 0 ? 0 : (causal ? p_first + 1 : s.len);
+            const int full_low = W && p_last + 1 > W ? p_last + 1 - W : 0;
+            const int step_end = st.steps < unit1 * WAVES ? st.steps : unit1 * WAVES;
+
+            const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
+            const char *kb = static_cast<const char *>(C.k_pages) + (long)kvh * HD * ES;
+            const char *vb = static_cast<const char *>(C.v_pages) + (long)kvh * HD * ES;
+
+            float m[RT], l[RT];
+            f32x4 acc[RT][NE];
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) {
-                const uint32_t seen = (seen_bits(pos[rt], key0, s.len, A.attn) & there) >> (8 * g);
+                m[rt] = -INFINITY;
+                l[rt] = 0.f;
 #pragma unroll
-                for (int t = 0; t < 2; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) sc[rt][t][i] = (seen >> (4 * t + i)) & 1u ? sc[rt][t][i] : -INFINITY;
+                for (int e = 0; e < NE; ++e) acc[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
             }
-            const uint32_t any = (first_bits(high - key0) & (~first_bits(low - key0) | first_bits(sink - key0)) & there) >> (8 * g);
-            bool bad = false;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int w = 0; w < NE / 2; ++w) {
-                    vw[j][w] = (any >> j) & 1u ? vw[j][w] : 0u;
-                    bad |= not_finite(T{}, vw[j][w]);
-                }
-            odd = __any(bad);
-        }
 
-        // softmax of the step, and the weights as operands: the leading 16-bit term and the next
-        u32x4 ph[RT], pl[RT];
+            auto key_of = [&](int u) { return (u < st.s_steps ? u : st.first + u - st.s_steps) * STEP; };
+            // the page of step u's positions (of position key + lane % 32, where pages end inside a step), or -1
+            auto page_of = [&](int u) {
+                const int j = key_of(u) + (whole ? 0 : (lane & 31));
+                return j < high ? table[j / C.page_size] : 0;
+            };
+            struct Raw {
+                uint4 k[2][NL];
+                Words<NE * ES / 4> v[8];
+                uint32_t there;                // positions whose page is there
+            };
+            // requests step u's keys and values: the lane's share of K, entries of two positions, and of V, entries NE r16 .. of
+            // positions key0 + 8 g .. + 7
+            auto request = [&](int u, int page, Raw &f) {
+                const int key0 = key_of(u);
+                const bool ok = page >= 0 && page < C.n_pages;
+                if (!ok) atomicOr(A.err_flag, ERR_PAGE);
+                if (whole) {
+                    f.there = ok ? 0xffffffffu : 0u;
+                    if (!ok) return;
+                    const long at = ((long)page * C.page_size + key0 % C.page_size) * pitch;
+                    const char *kp = kb + at + (int)(8 * (r16 >> 2) + (r16 & 3)) * pitch + 16 * g, *vp = vb + at + 8 * g * pitch + NE * ES * r16;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            float mx = m[rt];
+                    for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[rt][0][i], sc[rt][1][i]));
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float ref = mx == -INFINITY ? 0.f : mx * c2;
-            if (__any(mx > m[rt])) {
-                const float alpha = exp2f(m[rt] * c2 - ref);
-                l[rt] *= alpha;
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = *reinterpret_cast<const uint4 *>(kp + 4 * t * pitch + 64 * c);
 #pragma unroll
-                for (int e = 0; e < NE; ++e) acc[rt][e] *= alpha;
-            }
-            m[rt] = mx;
-            float sum = 0.f;
+                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vp + j * pitch);
+                } else {
+                    const int j0 = key0 + (lane & 31);
+                    const int slot = ok && j0 < high ? page * C.page_size + j0 % C.page_size : 0;
+                    f.there = (uint32_t)__ballot(ok);
 #pragma unroll
-            for (int t = 0; t < 2; ++t)
+                    for (int t = 0; t < 2; ++t) {
+                        const char *kp = kb + __shfl(slot, 8 * (r16 >> 2) + 4 * t + (r16 & 3)) * pitch + 16 * g;
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    const float p0 = exp2f(fmaf(sc[rt][t][i], c2, -ref)), p1 = exp2f(fmaf(sc[rt][t][i + 1], c2, -ref));
-                    float r0, r1, x, y;
-                    sum += p0 + p1;
-                    ph[rt][2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
-                    pl[rt][2 * t + i / 2] = pack2(T{}, r0, r1, x, y);
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = *reinterpret_cast<const uint4 *>(kp + 64 * c);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vb + __shfl(slot, 8 * g + j) * pitch + NE * ES * r16);
                 }
-            l[rt] += sum;
-        }
+            };
 
-        if (!odd) {
+            auto compute = [&](int u, const Raw &f) {
+                const int key0 = key_of(u);
+                const uint32_t there = f.there;
+                if (there == 0) return;
+                const bool partial = there != 0xffffffffu || key0 + STEP > full_high || (key0 < full_low && key0 + STEP > sink);
+                f32x4 sc[RT][2];
 #pragma unroll
-            for (int e = 0; e < NE; ++e) {
-                u32x4 vt;
+                for (int t = 0; t < 2; ++t) {
+                    u32x4 kf[NC];
+                    if constexpr (E8) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    vt[k] = __builtin_amdgcn_perm(vw[2 * k + 1][e / 2], vw[2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+                        for (int c = 0; c < NL; ++c) {
+                            uint32_t a0, a1, a2, a3;
+                            widen(T{}, f.k[t][c].x, a0, a1);
+                            widen(T{}, f.k[t][c].y, a2, a3);
+                            kf[2 * c] = u32x4{a0, a1, a2, a3};
+                            widen(T{}, f.k[t][c].z, a0, a1);
+                            widen(T{}, f.k[t][c].w, a2, a3);
+                            kf[2 * c + 1] = u32x4{a0, a1, a2, a3};
+                        }
+                    } else {
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    acc[rt][e] = mfma(T{}, vt, ph[rt], acc[rt][e]);
-                    acc[rt][e] = mfma(T{}, vt, pl[rt], acc[rt][e]);
-                }
-            }
-        } else {
-            // a weight of zero times such a value is not zero: row by row, with the values that the row sees
-            for (int rr = 0; rr < 16; ++rr)
+                        for (int c = 0; c < NC; ++c) kf[c] = u32x4{f.k[t][c].x, f.k[t][c].y, f.k[t][c].z, f.k[t][c].w};
+                    }
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    const uint32_t keep = seen_bits(__shfl(pos[rt], rr), key0, s.len, A.attn) >> (8 * g);
+                    for (int rt = 0; rt < RT; ++rt) {
+                        sc[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < NE; ++e) {
-                        u32x4 vt;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            vt[k] = __builtin_amdgcn_perm(vw[2 * k + 1][e / 2], vw[2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u) &
-                                    (((keep >> (2 * k)) & 1u ? 0xffffu : 0u) | ((keep >> (2 * k + 1)) & 1u ? 0xffff0000u : 0u));
-                        const f32x4 d = mfma(T{}, vt, pl[rt], mfma(T{}, vt, ph[rt], f32x4{0.f, 0.f, 0.f, 0.f}));
-                        if (r16 == rr) acc[rt][e] += d;
+                        for (int c = 0; c < NC; ++c) sc[rt][t] = mfma(T{}, kf[c], qf[rt][c], sc[rt][t]);
                     }
                 }
-        }
-    }
-
-    // the four lanes of a row add up their sums, the waves their rows
+                uint32_t vw[8][NE / 2];
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        l[rt] += __shfl_xor(l[rt], 16);
-        l[rt] += __shfl_xor(l[rt], 32);
-        if (g == 0) {
-            sm[wave][16 * rt + r16] = m[rt];
-            sl[wave][16 * rt + r16] = l[rt];
-        }
-    }
-    const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
-    for (int rt = 0; rt < RT; ++rt) {
-        __syncthreads();
-        {
-            float mx = -INFINITY;
+                for (int j = 0; j < 8; ++j) {
+                    if constexpr (E8) {
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + r16]);
-            float mine = 0.f;
-            f32x4 a[NE];
+                        for (int w = 0; w < NE / 4; ++w) widen(T{}, f.v[j].w[w], vw[j][2 * w], vw[j][2 * w + 1]);
+                    } else {
 #pragma unroll
-            for (int q = 0; q < RT; ++q)
-                if (q == rt) {
-                    mine = m[q];
-#pragma unroll
-                    for (int e = 0; e < NE; ++e) a[e] = acc[q][e];
+                        for (int w = 0; w < NE / 2; ++w) vw[j][w] = f.v[j].w[w];
+                    }
                 }
-            const float f = mine == -INFINITY ? 0.f : exp2f((mine - mx) * c2);
+
+                if (partial) {
+                    // scores of positions that a row does not see are dropped
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const uint32_t seen = (seen_bits(pos[rt], key0, s.len, A.attn) & there) >> (8 * g);
 #pragma unroll
-                for (int e = 0; e < NE; e += 4)
-                    *reinterpret_cast<float4 *>(&so[wave][r16][NE * (4 * g + i) + e]) =
-                        make_float4(a[e][i] * f, a[e + 1][i] * f, a[e + 2][i] * f, a[e + 3][i] * f);
+                        for (int t = 0; t < 2; ++t)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) sc[rt][t][i] = (seen >> (4 * t + i)) & 1u ? sc[rt][t][i] : -INFINITY;
+                    }
+                }
+
+                // softmax of the step, and the weights as operands: the leading 16-bit term and the next
+                u32x4 ph[RT], pl[RT];
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                    float mx = m[rt];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[rt][0][i], sc[rt][1][i]));
+                    mx = fmaxf(mx, __shfl_xor(mx, 16));
+                    mx = fmaxf(mx, __shfl_xor(mx, 32));
+                    const float ref = mx == -INFINITY ? 0.f : mx * c2;
+                    if (__any(mx > m[rt])) {
+                        const float alpha = exp2f(m[rt] * c2 - ref);
+                        l[rt] *= alpha;
+#pragma unroll
+                        for (int e = 0; e < NE; ++e) acc[rt][e] *= alpha;
+                    }
+                    m[rt] = mx;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; i += 2) {
+                            const float p0 = exp2f(fmaf(sc[rt][t][i], c2, -ref)), p1 = exp2f(fmaf(sc[rt][t][i + 1], c2, -ref));
+                            float r0, r1, x, y;
+                            sum += p0 + p1;
+                            ph[rt][2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
+                            pl[rt][2 * t + i / 2] = pack2(T{}, r0, r1, x, y);
+                        }
+                    l[rt] += sum;
+                }
+
+                if (partial) {
+                    // a weight of zero times a value that is not finite is not zero: such values leave the product where only some
+                    // rows see them, and are added to those rows by themselves
+                    const uint32_t any = first_bits(high - key0) & (~first_bits(low - key0) | first_bits(sink - key0)) & there;
+                    bool bad = false;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int w = 0; w < NE / 2; ++w) {
+                            vw[j][w] = (any >> (8 * g + j)) & 1u ? vw[j][w] : 0u;
+                            bad |= not_finite(T{}, vw[j][w]);
+                        }
+                    if (__any(bad)) {
+                        uint32_t *const vl = reinterpret_cast<uint32_t *>(&so[wave][0][0]);      // [32][HD / 2]: the step's values
+                        uint16_t *const wl = sw[wave];                                           // [32][16 RT]: its weights
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+#pragma unroll
+                            for (int w = 0; w < NE / 2; ++w) {
+                                vl[(8 * g + j) * (HD / 2) + NE / 2 * r16 + w] = vw[j][w];
+                                vw[j][w] = finite_halves(T{}, vw[j][w]);
+                            }
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) wl[(8 * g + j) * 16 * RT + 16 * rt + r16] = (uint16_t)(j & 1 ? ph[rt][j / 2] >> 16 : ph[rt][j / 2]);
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+                        for (int k = 0; k < 32; ++k) {
+                            if (!((any >> k) & 1u)) continue;
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                                for (int w = 0; w < NE / 2; ++w) {
+                                    const uint32_t v = vl[k * (HD / 2) + NE / 2 * (4 * g + i) + w];
+                                    if (!not_finite(T{}, v)) continue;
+#pragma unroll
+                                    for (int rt = 0; rt < RT; ++rt) {
+                                        if (!((seen_bits(pos[rt], key0, s.len, A.attn) >> k) & 1u)) continue;
+                                        const float weight = to_float(T{}, wl[k * 16 * RT + 16 * rt + r16]);
+                                        if (not_finite(T{}, v & 0xffffu)) acc[rt][2 * w][i] += weight * to_float(T{}, v & 0xffffu);
+                                        if (not_finite(T{}, v >> 16)) acc[rt][2 * w + 1][i] += weight * to_float(T{}, v >> 16);
+                                    }
+                                }
+                        }
+                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                        __builtin_amdgcn_wave_barrier();
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    u32x4 vt;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        vt[k] = __builtin_amdgcn_perm(vw[2 * k + 1][e / 2], vw[2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        acc[rt][e] = mfma(T{}, vt, ph[rt], acc[rt][e]);
+                        if constexpr (RT <= 2) acc[rt][e] = mfma(T{}, vt, pl[rt], acc[rt][e]);
+                    }
+                }
+            };
+
+            {
+                int u = unit0 * WAVES + wave;
+                int page1 = u < step_end ? page_of(u) : 0, page2 = u + WAVES < step_end ? page_of(u + WAVES) : 0;
+                if constexpr (AHEAD) {
+                    Raw f;
+                    if (u < step_end) request(u, page1, f);
+                    for (; u < step_end; u += WAVES) {
+                        Raw next;
+                        const bool more = u + WAVES < step_end;
+                        if (more) request(u + WAVES, page2, next);
+                        if (u + 2 * WAVES < step_end) page2 = page_of(u + 2 * WAVES);
+                        compute(u, f);
+                        if (more) f = next;
+                    }
+                } else {
+                    for (; u < step_end; u += WAVES) {
+                        Raw f;
+                        request(u, page1, f);
+                        page1 = page2;
+                        if (u + 2 * WAVES < step_end) page2 = page_of(u + 2 * WAVES);
+                        compute(u, f);
+                    }
+                }
+            }
+
+            // the four lanes of a row add up their sums, the waves their rows
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                l[rt] += __shfl_xor(l[rt], 16);
+                l[rt] += __shfl_xor(l[rt], 32);
+                if (g == 0) {
+                    sm[wave][16 * rt + r16] = m[rt];
+                    sl[wave][16 * rt + r16] = l[rt];
+                }
+            }
+            const bool all = unit0 == 0 && unit1 == units;
+            float *const place = all ? nullptr : scratch + ((size_t)blockIdx.x * 2 + (unit0 == 0 ? 1 : 0)) * place_floats(P.rows, HD);
+            const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                __syncthreads();
+                {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + r16]);
+                    const float f = m[rt] == -INFINITY ? 0.f : exp2f((m[rt] - mx) * c2);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < NE; e += 4)
+                            *reinterpret_cast<float4 *>(&so[wave][r16][NE * (4 * g + i) + e]) =
+                                make_float4(acc[rt][e][i] * f, acc[rt][e + 1][i] * f, acc[rt][e + 2][i] * f, acc[rt][e + 3][i] * f);
+                }
+                __syncthreads();
+                const int rr = threadIdx.x >> 4, part = threadIdx.x & 15, r = row0 + 16 * rt + rr;
+                if (r < nr) {
+                    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + rr]);
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w)
+                        if (sm[w][16 * rt + rr] != -INFINITY) sum += sl[w][16 * rt + rr] * exp2f((sm[w][16 * rt + rr] - mx) * c2);
+                    float o[NE];
+#pragma unroll
+                    for (int e = 0; e < NE; ++e)
+                        o[e] = ((so[0][rr][NE * part + e] + so[1][rr][NE * part + e]) + so[2][rr][NE * part + e]) + so[3][rr][NE * part + e];
+                    if (all) {
+                        const int t = r / G;
+                        store_row<T, HD>(A, s.begin + t, kvh * G + r - t * G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
+                    } else {
+                        float4 *dst = reinterpret_cast<float4 *>(place + (size_t)(16 * rt + rr) * HD + NE * part);
+#pragma unroll
+                        for (int e = 0; e < NE; e += 4) dst[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        if (part == 0) *reinterpret_cast<float2 *>(place + (size_t)P.rows * HD + 2 * (16 * rt + rr)) = make_float2(mx, sum);
+                    }
+                }
+            }
         }
-        __syncthreads();
-        const int rr = threadIdx.x >> 4, part = threadIdx.x & 15, r = row0 + 16 * rt + rr;
-        if (r < nr) {
-            float mx = -INFINITY, sum = 0.f;
+        base += cost;
+        if (cur >= end) return;
+    }
+}
+
+// Adds up the pieces of an item that several workgroups had a part in, in the order of its positions: 16 threads a row
+template <typename T, bool E8, int HD>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend A, const Split P, const float *scratch) {
+    constexpr int NE = HD / 16;
+    __shared__ long tmp[2][4];
+    const mrp_paged_cache &C = A.cache;
+    const long cap = (long)C.max_pages * C.page_size;
+    const int b = blockIdx.y;
+    const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
+    const int nr = s.n * A.G, tiles = (nr + P.rows - 1) / P.rows;
+    if ((int)blockIdx.x >= tiles * C.n_kv_heads) return;
+    long total = 0, before = 0;
+    for (int i = threadIdx.x; i < A.rows.B; i += 256) {
+        const long c = cost_of(A, P, seq_rows(A.rows, A.n_rows, cap, i));
+        total += c;
+        if (i < b) before += c;
+    }
+    total = block_sum(total, tmp[0]);
+    before = block_sum(before, tmp[1]);
+    const int units = units_of(A, s), n = ranges(P, total);
+    const long i0 = before + (long)blockIdx.x * units, i1 = i0 + units;
+    // the workgroups of the item's first and last unit
+    auto owner = [&](long x) {
+        int w = (int)((double)x / (double)total * n);
+        w = w < 0 ? 0 : (w > n - 1 ? n - 1 : w);
+        while (w > 0 && range_begin(total, n, w) > x) --w;
+        while (w < n - 1 && range_begin(total, n, w + 1) <= x) ++w;
+        return w;
+    };
+    const int w0 = owner(i0), w1 = owner(i1 - 1);
+    if (w0 == w1) return;
+    const int kvh = blockIdx.x / tiles, row0 = blockIdx.x % tiles * P.rows;
+    const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
+    const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
+    const size_t size = place_floats(P.rows, HD);
+    const int rows = nr - row0 < P.rows ? nr - row0 : P.rows, part = threadIdx.x & 15;
+    for (int rr = threadIdx.x >> 4; rr < rows; rr += 16) {
+        float mx = -INFINITY, sum = 0.f, o[NE];
+        for (int w = w0; w <= w1; ++w)
+            mx = fmaxf(mx, scratch[(2 * (size_t)w + (w == w0)) * size + (size_t)P.rows * HD + 2 * rr]);
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + rr]);
+        for (int e = 0; e < NE; ++e) o[e] = 0.f;
+        for (int w = w0; w <= w1; ++w) {
+            const float *p = scratch + (2 * (size_t)w + (w == w0)) * size;
+            const float2 ml = *reinterpret_cast<const float2 *>(p + (size_t)P.rows * HD + 2 * rr);
+            const float f = ml.x == -INFINITY ? 0.f : exp2f((ml.x - mx) * c2);
+            sum += f * ml.y;
+            const float4 *src = reinterpret_cast<const float4 *>(p + (size_t)rr * HD + NE * part);
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w)
-                if (sm[w][16 * rt + rr] != -INFINITY) sum += sl[w][16 * rt + rr] * exp2f((sm[w][16 * rt + rr] - mx) * c2);
-            const float f = mx == -INFINITY ? 0.f : v_scale / sum;
-            const int t = r / G;
-            const long row = s.begin + t, h = kvh * G + r - t * G;
-            float o[NE];
-#pragma unroll
-            for (int e = 0; e < NE; ++e)
-                o[e] = mx == -INFINITY ? 0.f
-                                       : (((so[0][rr][NE * part + e] + so[1][rr][NE * part + e]) + so[2][rr][NE * part + e]) + so[3][rr][NE * part + e]) * f;
-            uint32_t *dst = reinterpret_cast<uint32_t *>(A.out + (row * A.attn.n_heads + h) * HD + NE * part);
-            float x, y;
-#pragma unroll
-            for (int e = 0; e < NE; e += 2) dst[e / 2] = pack2(T{}, o[e], o[e + 1], x, y);
-            if (A.lse && part == 0) A.lse[row * A.attn.n_heads + h] = mx == -INFINITY ? -INFINITY : mx * c2 * 0.6931471805599453f + logf(sum);
+            for (int e = 0; e < NE; e += 4) {
+                const float4 v = src[e / 4];
+                o[e] += f * v.x; o[e + 1] += f * v.y; o[e + 2] += f * v.z; o[e + 3] += f * v.w;
+            }
         }
+        const int r = row0 + rr, t = r / A.G;
+        store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
     }
 }
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
+// Rows of a tile: the fewest that hold a sequence's rows, up to 64 (32 of 256 entries: registers)
+int tile_rows(long rows, int HD) { return rows <= 16 ? 16 : (rows <= 32 || HD == 256 ? 32 : 64); }
+
+// The largest number of workgroups is what fits the device at once: two a compute unit for 16 rows of up to 128 entries, else one
+Split split_of(long rows, int HD, int nCU) {
+    const int tr = tile_rows(rows, HD);
+    return Split{tr, 1, (tr == 16 && HD <= 128 ? 2 : 1) * (nCU > 0 ? nCU : 1)};
+}
+
 template <typename T, bool E8, int HD>
-void launch(const Attend &a, hipStream_t st) {
-    const long rows = (long)a.G * (a.rows.max_new < a.n_rows ? a.rows.max_new : a.n_rows);
-    if (rows <= 16)
-        paged_attention_kernel<T, E8, HD, 1><<<dim3(1, a.cache.n_kv_heads, a.rows.B), 64 * WAVES, 0, st>>>(a);
-    else if (rows <= 32 || HD == 256)
-        paged_attention_kernel<T, E8, HD, 2><<<dim3(ceil_div(rows, 32), a.cache.n_kv_heads, a.rows.B), 64 * WAVES, 0, st>>>(a);
-    else if constexpr (HD < 256)
-        paged_attention_kernel<T, E8, HD, 4><<<dim3(ceil_div(rows, 64), a.cache.n_kv_heads, a.rows.B), 64 * WAVES, 0, st>>>(a);
+void launch(const Attend &a, const Split &p, float *scratch, hipStream_t st) {
+    constexpr bool AH = false;
+    if (p.rows == 16) paged_attention_kernel<T, E8, HD, 1, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
+    else if (p.rows == 32) paged_attention_kernel<T, E8, HD, 2, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
+    else if constexpr (HD < 256) paged_attention_kernel<T, E8, HD, 4, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
+    const int tiles = ceil_div(most_rows(a.n_rows, a.rows, a.G), p.rows);
+    paged_attention_join_kernel<T, E8, HD><<<dim3(tiles * a.cache.n_kv_heads, a.rows.B), 256, 0, st>>>(a, p, scratch);
 }
 
 template <typename T, bool E8>
-void launch_hd(const Attend &a, hipStream_t st) {
-    if (a.cache.head_dim == 64) launch<T, E8, 64>(a, st);
-    else if (a.cache.head_dim == 128) launch<T, E8, 128>(a, st);
-    else launch<T, E8, 256>(a, st);
+void launch_hd(const Attend &a, const Split &p, float *scratch, hipStream_t st) {
+    if (a.cache.head_dim == 64) launch<T, E8, 64>(a, p, scratch, st);
+    else if (a.cache.head_dim == 128) launch<T, E8, 128>(a, p, scratch, st);
+    else launch<T, E8, 256>(a, p, scratch, st);
 }
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -429,8 +557,15 @@ extern "C" {
 
 size_t mrp_paged_attention_scratch_bytes(const mrp_ctx *c, long n_rows, const mrp_new_rows *rows, const mrp_paged_cache *cache,
                                          const mrp_attn *attn) {
-    (void)c; (void)n_rows; (void)rows; (void)cache; (void)attn;
-    return 0;
+    if (!c || !rows || !cache || !attn || n_rows <= 0 || rows->B <= 0 || rows->max_new <= 0 || cache->n_kv_heads <= 0 ||
+        attn->n_heads < cache->n_kv_heads)
+        return 0;
+    const long per_head = most_rows(n_rows, *rows, attn->n_heads / cache->n_kv_heads);
+    if (prompt_takes(per_head, cache->head_dim))
+        return prompt_scratch_floats(per_head, rows->B, cache->n_kv_heads, (long)cache->max_pages * cache->page_size, cache->head_dim,
+                                     ctx_view(c).nCU) * sizeof(float);
+    const Split p = split_of(per_head, cache->head_dim, ctx_view(c).nCU);
+    return 2 * (size_t)p.workgroups * place_floats(p.rows, cache->head_dim) * sizeof(float);
 }
 
 int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_rows *rows, const mrp_paged_cache *cache,
@@ -442,7 +577,7 @@ int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_row
     CHECK(check_cache(c, what, cache));
     if (attn->n_heads < 1 || attn->n_heads > 1024 || attn->n_heads % cache->n_kv_heads)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %d heads over %d key heads", what, attn->n_heads, cache->n_kv_heads);
-    if (n_rows * (attn->n_heads / cache->n_kv_heads) > (1L << 26))
+    if (n_rows * attn->n_heads > (1L << 28))
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %ld rows of %d heads are too many", what, n_rows, attn->n_heads);
     if ((attn->dtype != MRP_DTYPE_BF16 && attn->dtype != MRP_DTYPE_F16) || (cache->dtype != MRP_DTYPE_E4M3 && cache->dtype != attn->dtype))
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: no form for type %d over a cache of type %d", what, attn->dtype, cache->dtype);
@@ -461,9 +596,15 @@ int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_row
     const Attend a = {*rows, *cache, *attn, (int)n_rows, attn->n_heads / cache->n_kv_heads, static_cast<const uint16_t *>(q), q_stride,
                       static_cast<uint16_t *>(out), lse, ctx_view(c).err_flag};
     hipStream_t st = static_cast<hipStream_t>(stream);
+    if (prompt_takes(most_rows(n_rows, *rows, a.G), cache->head_dim)) {
+        const hipError_t e = launch_prompt_attention(a, static_cast<float *>(scratch), ctx_view(c).nCU, st);
+        return e == hipSuccess ? MRP_OK : ctx_fail(c, MRP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+    }
     const bool e8 = cache->dtype == MRP_DTYPE_E4M3;
-    if (attn->dtype == MRP_DTYPE_BF16) e8 ? launch_hd<BF16, true>(a, st) : launch_hd<BF16, false>(a, st);
-    else e8 ? launch_hd<F16, true>(a, st) : launch_hd<F16, false>(a, st);
+    const Split p = split_of(most_rows(n_rows, *rows, a.G), cache->head_dim, ctx_view(c).nCU);
+    float *const s = static_cast<float *>(scratch);
+    if (attn->dtype == MRP_DTYPE_BF16) e8 ? launch_hd<BF16, true>(a, p, s, st) : launch_hd<BF16, false>(a, p, s, st);
+    else e8 ? launch_hd<F16, true>(a, p, s, st) : launch_hd<F16, false>(a, p, s, st);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? MRP_OK : ctx_fail(c, MRP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
