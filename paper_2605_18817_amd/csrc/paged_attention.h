@@ -9,6 +9,9 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
+// 2^x to one unit in the last place; below 2^-126: 0
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
 __device__ __forceinline__ f32x4 mfma(BF16, u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
@@ -43,14 +46,19 @@ __device__ __forceinline__ bool not_finite(T, uint32_t v) {   // either half
     return (v & E) == E || ((v >> 16) & E) == E;
 }
 
-__device__ __forceinline__ float to_float(BF16, uint32_t half) { return __uint_as_float(half << 16); }
-__device__ __forceinline__ float to_float(F16, uint32_t half) { return (float)__builtin_bit_cast(_Float16, (uint16_t)half); }
+__device__ __forceinline__ constexpr uint32_t one_bits(BF16) { return 0x3f80u; }
+__device__ __forceinline__ constexpr uint32_t one_bits(F16) { return 0x3c00u; }
 template <typename T>
 __device__ __forceinline__ uint32_t finite_halves(T, uint32_t v) {   // halves that are not finite cleared
     constexpr uint32_t E = __is_same(T, BF16) ? 0x7f80u : 0x7c00u;
     if ((v & E) == E) v &= 0xffff0000u;
     if (((v >> 16) & E) == E) v &= 0xffffu;
     return v;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t odd_halves(T, uint32_t v) {      // 1 for halves that are not finite, else 0
+    constexpr uint32_t E = __is_same(T, BF16) ? 0x7f80u : 0x7c00u;
+    return ((v & E) == E ? one_bits(T{}) : 0u) | (((v >> 16) & E) == E ? one_bits(T{}) << 16 : 0u);
 }
 
 struct Attend {

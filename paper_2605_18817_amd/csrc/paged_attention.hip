@@ -70,7 +70,6 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
     constexpr int NL = E8 ? NC / 2 : NC;       // 16-byte pieces of a lane's share of K
     __shared__ float sm[WAVES][16 * RT], sl[WAVES][16 * RT];
     __shared__ __align__(16) float so[WAVES][16][HD + 4];
-    __shared__ uint16_t sw[WAVES][32 * 16 * RT];
     __shared__ long scan[WAVES];
     __shared__ long seq_base;
     __shared__ int seq_at;
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     mx = fmaxf(mx, __shfl_xor(mx, 32));
                     const float ref = mx == -INFINITY ? 0.f : mx * c2;
                     if (__any(mx > m[rt])) {
-                        const float alpha = exp2f(m[rt] * c2 - ref);
+                        const float alpha = exp2_(m[rt] * c2 - ref);
                         l[rt] *= alpha;
 #pragma unroll
                         for (int e = 0; e < NE; ++e) acc[rt][e] *= alpha;
@@ -298,7 +297,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
                         for (int i = 0; i < 4; i += 2) {
-                            const float p0 = exp2f(fmaf(sc[rt][t][i], c2, -ref)), p1 = exp2f(fmaf(sc[rt][t][i + 1], c2, -ref));
+                            const float p0 = exp2_(fmaf(sc[rt][t][i], c2, -ref)), p1 = exp2_(fmaf(sc[rt][t][i + 1], c2, -ref));
                             float r0, r1, x, y;
                             sum += p0 + p1;
                             ph[rt][2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
@@ -307,61 +306,53 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     l[rt] += sum;
                 }
 
-                if (partial) {
-                    // a weight of zero times a value that is not finite is not zero: such values leave the product where only some
-                    // rows see them, and are added to those rows by themselves
-                    const uint32_t any = first_bits(high - key0) & (~first_bits(low - key0) | first_bits(sink - key0)) & there;
-                    bool bad = false;
+                bool bad = false;
+                if (partial) {                     // values that no row sees are cleared
+                    const uint32_t any = (first_bits(high - key0) & (~first_bits(low - key0) | first_bits(sink - key0)) & there) >> (8 * g);
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
 #pragma unroll
                         for (int w = 0; w < NE / 2; ++w) {
-                            vw[j][w] = (any >> (8 * g + j)) & 1u ? vw[j][w] : 0u;
+                            vw[j][w] = (any >> j) & 1u ? vw[j][w] : 0u;
                             bad |= not_finite(T{}, vw[j][w]);
                         }
-                    if (__any(bad)) {
-                        uint32_t *const vl = reinterpret_cast<uint32_t *>(&so[wave][0][0]);      // [32][HD / 2]: the step's values
-                        uint16_t *const wl = sw[wave];                                           // [32][16 RT]: its weights
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-#pragma unroll
-                            for (int w = 0; w < NE / 2; ++w) {
-                                vl[(8 * g + j) * (HD / 2) + NE / 2 * r16 + w] = vw[j][w];
-                                vw[j][w] = finite_halves(T{}, vw[j][w]);
-                            }
-#pragma unroll
-                            for (int rt = 0; rt < RT; ++rt) wl[(8 * g + j) * 16 * RT + 16 * rt + r16] = (uint16_t)(j & 1 ? ph[rt][j / 2] >> 16 : ph[rt][j / 2]);
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-                        for (int k = 0; k < 32; ++k) {
-                            if (!((any >> k) & 1u)) continue;
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                                for (int w = 0; w < NE / 2; ++w) {
-                                    const uint32_t v = vl[k * (HD / 2) + NE / 2 * (4 * g + i) + w];
-                                    if (!not_finite(T{}, v)) continue;
-#pragma unroll
-                                    for (int rt = 0; rt < RT; ++rt) {
-                                        if (!((seen_bits(pos[rt], key0, s.len, A.attn) >> k) & 1u)) continue;
-                                        const float weight = to_float(T{}, wl[k * 16 * RT + 16 * rt + r16]);
-                                        if (not_finite(T{}, v & 0xffffu)) acc[rt][2 * w][i] += weight * to_float(T{}, v & 0xffffu);
-                                        if (not_finite(T{}, v >> 16)) acc[rt][2 * w + 1][i] += weight * to_float(T{}, v >> 16);
-                                    }
-                                }
-                        }
-                        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                        __builtin_amdgcn_wave_barrier();
-                    }
+                    bad = __any(bad);
                 }
-#pragma unroll
-                for (int e = 0; e < NE; ++e) {
+                // entry e of the lanes' shares as an A operand
+                auto turned = [&](int e) {
                     u32x4 vt;
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         vt[k] = __builtin_amdgcn_perm(vw[2 * k + 1][e / 2], vw[2 * k][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
+                    return vt;
+                };
+                if (bad) {
+                    // A weight of zero times a value that is not finite is not zero.  Such values leave the product; how many of them a
+                    // row sees in an entry is a product too, of ones, and makes the row's entry NaN
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const uint32_t seen = seen_bits(pos[rt], key0, s.len, A.attn) >> (8 * g);
+                        u32x4 sees;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) sees[j] = ((seen >> (2 * j)) & 1u) * one_bits(T{}) + (((seen >> (2 * j + 1)) & 1u) * one_bits(T{}) << 16);
+#pragma unroll
+                        for (int e = 0; e < NE; ++e) {
+                            u32x4 other = turned(e);
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) other[k] = odd_halves(T{}, other[k]);
+                            const f32x4 count = mfma(T{}, other, sees, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) acc[rt][e][i] = count[i] > 0.f ? NAN : acc[rt][e][i];
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+#pragma unroll
+                        for (int w = 0; w < NE / 2; ++w) vw[j][w] = finite_halves(T{}, vw[j][w]);
+                }
+#pragma unroll
+                for (int e = 0; e < NE; ++e) {
+                    const u32x4 vt = turned(e);
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
                         acc[rt][e] = mfma(T{}, vt, ph[rt], acc[rt][e]);
@@ -415,7 +406,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     float mx = -INFINITY;
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + r16]);
-                    const float f = m[rt] == -INFINITY ? 0.f : exp2f((m[rt] - mx) * c2);
+                    const float f = m[rt] == -INFINITY ? 0.f : exp2_((m[rt] - mx) * c2);
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -431,7 +422,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + rr]);
 #pragma unroll
                     for (int w = 0; w < WAVES; ++w)
-                        if (sm[w][16 * rt + rr] != -INFINITY) sum += sl[w][16 * rt + rr] * exp2f((sm[w][16 * rt + rr] - mx) * c2);
+                        if (sm[w][16 * rt + rr] != -INFINITY) sum += sl[w][16 * rt + rr] * exp2_((sm[w][16 * rt + rr] - mx) * c2);
                     float o[NE];
 #pragma unroll
                     for (int e = 0; e < NE; ++e)
@@ -498,7 +489,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend 
         for (int w = w0; w <= w1; ++w) {
             const float *p = scratch + (2 * (size_t)w + (w == w0)) * size;
             const float2 ml = *reinterpret_cast<const float2 *>(p + (size_t)P.rows * HD + 2 * rr);
-            const float f = ml.x == -INFINITY ? 0.f : exp2f((ml.x - mx) * c2);
+            const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - mx) * c2);
             sum += f * ml.y;
             const float4 *src = reinterpret_cast<const float4 *>(p + (size_t)rr * HD + NE * part);
 #pragma unroll

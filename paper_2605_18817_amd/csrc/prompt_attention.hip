@@ -25,15 +25,29 @@ __device__ __forceinline__ f32x16 mfma32(F16, u32x4 a, u32x4 b, f32x16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
+template <bool B>
+struct Odd {
+    static constexpr bool value = B;
+};
+using Even = Odd<false>;
+
 struct Cut {
     int tiles;       // row tiles that a sequence can have
     int pieces;      // parts of the positions, joined by a second kernel where there is more than one
 };
 
-// Place of key x (0 .. 31) of a tile's half in shared memory
+typedef const __attribute__((address_space(1))) void *gas_ptr;
+typedef __attribute__((address_space(3))) void *las_ptr;
+
+// Row of key x (0 .. 31) of a tile's half in shared memory, and the key of a row
 __device__ __forceinline__ int key_row(int x) {
     const int i = 8 * (x >> 4) + (x & 7), h = (x >> 3) & 1;
     return 8 * (i >> 2) + 4 * h + (i & 3);
+}
+
+__device__ __forceinline__ int row_key(int y) {
+    const int i = 4 * (y >> 3) + (y & 3), h = (y >> 2) & 1;
+    return 16 * (i >> 3) + 8 * h + (i & 7);
 }
 
 // The tiles of a piece of a row tile
@@ -57,22 +71,36 @@ __device__ __forceinline__ uint32_t load_part(const char *p) {
     else return *reinterpret_cast<const uint16_t *>(p);
 }
 
+// Orders the N products and the N reads of their operands above: reads four products ahead
+template <int N>
+__device__ __forceinline__ void four_ahead() {
+    __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+    for (int i = 0; i < N - 4; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+}
+
 template <typename T, bool E8, int HD, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Attend A, const Cut P, float *scratch) {
     constexpr int ES = E8 ? 1 : 2, THREADS = 64 * NW, ROWS = 32 * NW;
     constexpr int NC = HD / 16;                   // contraction steps of a score
     constexpr int ND = HD / 32;                   // tiles of 32 entries of the output
-    constexpr int KROW = HD * 2 + 16;             // bytes of a key's row in shared memory: 16 more spread the rows over the banks
-    constexpr int VROW = KT * 2 + 16;             // ... and of an entry's
-    constexpr int KP = HD * ES / 16;              // 16-byte pieces of a key
+    constexpr int KROW = HD * 2;                  // bytes of a key's row in shared memory: piece x of row y lies in place x ^ y % KS,
+    constexpr int KS = KROW / 16;                 // which spreads a piece of eight rows over the banks
+    constexpr int VROW = KT * 2 + 16;             // bytes of an entry's: 16 more spread the rows
+    constexpr int KP = HD * ES / 16;              // 16-byte pieces of a key in the cache
     constexpr int KN = KT * KP < THREADS ? 1 : KT * KP / THREADS;   // of them for a thread
     constexpr bool K_ALL = KT * KP >= THREADS;    // ... for every thread
     constexpr int DW = E8 ? 4 : 2;                // entries of a value that a thread takes
     constexpr int VL = HD / DW;                   // threads on a value
     constexpr int VK = KT * VL / THREADS;         // keys of a thread
     static_assert(VK >= 2 && VK <= 16, "a thread's share");
-    __shared__ __align__(16) char ks[2][KT * KROW];
-    __shared__ __align__(16) char vs[2][HD * VROW];
+    // (two variables, and the loop takes the tiles in pairs: what is on its way into one is then seen not to touch the other)
+    __shared__ __align__(16) char ks_even[KT * KROW], ks_odd[KT * KROW];
+    __shared__ __align__(16) char vs_even[HD * VROW], vs_odd[HD * VROW];
     __shared__ int slots[4][KT];                  // places of the positions of four tiles, -1: not there
     __shared__ uint32_t there[4][2];
     __shared__ int odd[4];                        // the tile has values that are not finite where only some rows see them
@@ -136,15 +164,25 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             }
         }
     };
-    uint4 kreg[KN];
+    uint4 kreg[KN];                               // (8 bits: keys are widened on their way; else they go to shared memory directly)
     uint32_t vreg[VK];
     const int vd = tid % VL, vg = tid / VL;       // the thread's entries DW vd .., keys VK vg ..
-    auto request = [&](int i) {
+    auto request = [&](int i, auto odd_tile) {
         const int at = i & 3;
+        char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even;
+        if constexpr (E8) {
 #pragma unroll
-        for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
-            const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP, slot = slots[at][key];
-            kreg[n] = *reinterpret_cast<const uint4 *>(kb + (slot < 0 ? 0 : slot) * pitch + 16 * part);
+            for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
+                const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP, slot = slots[at][key];
+                kreg[n] = *reinterpret_cast<const uint4 *>(kb + (slot < 0 ? 0 : slot) * pitch + 16 * part);
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < KN; ++n) {        // 64 pieces of a wave lie side by side
+                const int first = (n * NW + wave) * 64, y = (first + lane) / KS, part = ((first + lane) % KS) ^ (y & (KS - 1));
+                const int slot = slots[at][(y & 32) + row_key(y & 31)];
+                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + (slot < 0 ? 0 : slot) * pitch + 16 * part), (las_ptr)(ks + 16 * first), 16, 0, 0);
+            }
         }
 #pragma unroll
         for (int n = 0; n < VK; ++n) {
@@ -152,22 +190,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             vreg[n] = load_part<DW * ES>(vb + (slot < 0 ? 0 : slot) * pitch + DW * ES * vd);
         }
     };
-    auto put = [&](int i) {
-        const int u = pc.begin + i, buf = i & 1, at = i & 3;
+    auto put = [&](int i, auto odd_tile) {
+        const int u = pc.begin + i, at = i & 3;
+        char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
+        if constexpr (E8) {
 #pragma unroll
-        for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
-            const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP;
-            char *to = ks[buf] + ((key & 32) + key_row(key & 31)) * KROW;
-            if constexpr (E8) {
+            for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
+                const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP, y = (key & 32) + key_row(key & 31);
+                char *to = ks + y * KROW;
                 uint32_t a0, a1, a2, a3, b0, b1, b2, b3;
                 widen(T{}, kreg[n].x, a0, a1);
                 widen(T{}, kreg[n].y, a2, a3);
                 widen(T{}, kreg[n].z, b0, b1);
                 widen(T{}, kreg[n].w, b2, b3);
-                reinterpret_cast<uint4 *>(to + 32 * part)[0] = make_uint4(a0, a1, a2, a3);
-                reinterpret_cast<uint4 *>(to + 32 * part)[1] = make_uint4(b0, b1, b2, b3);
-            } else {
-                *reinterpret_cast<uint4 *>(to + 16 * part) = kreg[n];
+                *reinterpret_cast<uint4 *>(to + 16 * ((2 * part) ^ (y & (KS - 1)))) = make_uint4(a0, a1, a2, a3);
+                *reinterpret_cast<uint4 *>(to + 16 * ((2 * part + 1) ^ (y & (KS - 1)))) = make_uint4(b0, b1, b2, b3);
             }
         }
         uint32_t w[VK][DW / 2];
@@ -179,7 +216,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         const int key0 = key_of(u);
         const uint32_t th0 = there[at][0], th1 = there[at][1];
         if (is_partial(key0, th0, th1)) {
-            // values that no row sees are cleared; those that only some rows see and are not finite too, and the tile is marked
+            // values that no row sees are cleared; the tile is marked where others are not finite
             bool bad = false;
 #pragma unroll
             for (int n = 0; n < VK; ++n) {
@@ -189,7 +226,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
                 for (int i = 0; i < DW / 2; ++i) {
                     const uint32_t v = any ? w[n][i] : 0u;
                     bad |= not_finite(T{}, v);
-                    w[n][i] = finite_halves(T{}, v);
+                    w[n][i] = v;
                 }
             }
             if (bad) odd[at] = 1;
@@ -200,7 +237,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
             for (int n = 0; n < VK / 2; ++n) col[n] = __builtin_amdgcn_perm(w[2 * n + 1][e / 2], w[2 * n][e / 2], e & 1 ? 0x07060302u : 0x05040100u);
             const int d = DW * vd + e;
-            char *to = vs[buf] + ((d & 1) * (HD / 2) + (d >> 1)) * VROW + 2 * VK * vg;
+            char *to = vs + ((d & 1) * (HD / 2) + (d >> 1)) * VROW + 2 * VK * vg;
             if constexpr (VK == 16) {
                 reinterpret_cast<uint4 *>(to)[0] = make_uint4(col[0], col[1], col[2], col[3]);
                 reinterpret_cast<uint4 *>(to)[1] = make_uint4(col[4], col[5], col[6], col[7]);
@@ -221,8 +258,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
-    auto compute = [&](int i) {
-        const int u = pc.begin + i, buf = i & 1, at = i & 3;
+    auto compute = [&](int i, auto odd_tile) {
+        const int u = pc.begin + i, at = i & 3;
+        char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         const int key0 = key_of(u);
         const uint32_t th0 = there[at][0], th1 = there[at][1];
         f32x16 sc[2];
@@ -232,10 +270,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             for (int i = 0; i < 16; ++i) sc[t][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const u32x4 a = *reinterpret_cast<const u32x4 *>(ks[buf] + (32 * t + r32) * KROW + 32 * c + 16 * h);
+                const u32x4 a = *reinterpret_cast<const u32x4 *>(ks + (32 * t + r32) * KROW + ((32 * c) ^ (16 * (h ^ (r32 & (KS - 1))))));
                 sc[t] = mfma32(T{}, a, qf[c], sc[t]);
             }
         }
+        four_ahead<2 * NC>();
         const bool partial = is_partial(key0, th0, th1);
         if (partial) {
 #pragma unroll
@@ -252,7 +291,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         // the sums are brought to a new reference where a score is more than a factor of 2^8 above the old one
         if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx > m))) {
             const float top = fmaxf(m, mx);
-            const float alpha = m == -INFINITY ? 0.f : exp2f((m - top) * c2);
+            const float alpha = m == -INFINITY ? 0.f : exp2_((m - top) * c2);
             m = top;
             l *= alpha;
 #pragma unroll
@@ -263,49 +302,57 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 32; i += 2) {
-            const float p0 = exp2f(fmaf(sc[i >> 4][i & 15], c2, -ref)), p1 = exp2f(fmaf(sc[i >> 4][(i & 15) + 1], c2, -ref));
+            const float p0 = exp2_(fmaf(sc[i >> 4][i & 15], c2, -ref)), p1 = exp2_(fmaf(sc[i >> 4][(i & 15) + 1], c2, -ref));
             float x, y;
             sum += p0 + p1;
             p[i >> 3][(i & 7) >> 1] = pack2(T{}, p0, p1, x, y);
         }
         l += sum;
         if (partial && odd[at]) {
-            // add what is not finite to the rows that see it, from the cache itself
+            // A weight of zero times a value that is not finite is not zero.  Such values leave the product; how many of them a row
+            // sees in an entry is a product too, of ones, and makes the row's entry NaN
+            u32x4 sees[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t seen = seen_bits(pos, key0 + 32 * (q >> 1), s.len, A.attn) >> (16 * (q & 1) + 8 * h);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-#pragma unroll 1
-                    for (int hh = 0; hh < 2; ++hh) {
-                        const int k = 16 * q + 8 * hh + j, slot = slots[at][k];
-                        const uint32_t two = __shfl(p[q][j / 2], 32 * hh + r32);
-                        const float weight = to_float(T{}, j & 1 ? two >> 16 : two & 0xffffu);
-                        const bool sees = slot >= 0 && ((seen_bits(pos, key0 + (k & 32), s.len, A.attn) >> (k & 31)) & 1u);
-                        if (!sees) continue;
+                for (int j = 0; j < 4; ++j) sees[q][j] = ((seen >> (2 * j)) & 1u) * one_bits(T{}) + (((seen >> (2 * j + 1)) & 1u) * one_bits(T{}) << 16);
+            }
 #pragma unroll
-                        for (int d = 0; d < ND; ++d)
+            for (int d = 0; d < ND; ++d) {
+                f32x16 count;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const int x = 32 * d + 8 * (i >> 2) + 4 * h + (i & 3), e = 2 * (x % (HD / 2)) + x / (HD / 2);
-                                uint32_t half;
-                                if constexpr (E8) {
-                                    uint32_t lo, hi;
-                                    widen(T{}, *reinterpret_cast<const uint8_t *>(vb + slot * pitch + e), lo, hi);
-                                    half = lo & 0xffffu;
-                                } else {
-                                    half = *reinterpret_cast<const uint16_t *>(vb + slot * pitch + 2 * e);
-                                }
-                                if (not_finite(T{}, half)) acc[d][i] += weight * to_float(T{}, half);
-                            }
-                    }
+                for (int i = 0; i < 16; ++i) count[i] = 0.f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 16 * h);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a[j] = odd_halves(T{}, a[j]);
+                    count = mfma32(T{}, a, sees[q], count);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[d][i] = count[i] > 0.f ? NAN : acc[d][i];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            __syncthreads();                      // (all waves are here: the mark is the tile's)
+            for (int x = tid; x < HD * (KT / 8); x += THREADS) {
+                u32x4 *const v = reinterpret_cast<u32x4 *>(vs + (x / (KT / 8)) * VROW + 16 * (x % (KT / 8)));
+                u32x4 a = *v;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) a[j] = finite_halves(T{}, a[j]);
+                *v = a;
+            }
+            __syncthreads();
         }
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const u32x4 a = *reinterpret_cast<const u32x4 *>(vs[buf] + (32 * d + r32) * VROW + 32 * q + 16 * h);
+                const u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 16 * h);
                 acc[d] = mfma32(T{}, a, p[q], acc[d]);
             }
+        four_ahead<4 * ND>();
     };
 
     // three tiles are on their way: the places of the one after the next, keys and values of the next, and the one at work
@@ -314,16 +361,23 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         look_up(0);
         if (n > 1) look_up(1);
         __syncthreads();
-        request(0);
-        put(0);
-        __syncthreads();
+        request(0, Even{});
+        put(0, Even{});
     }
-    for (int i = 0; i < n; ++i) {
-        if (i + 1 < n) request(i + 1);
+    __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): what goes to shared memory directly is there
+    __syncthreads();
+    auto step = [&](int i, auto odd_tile) {
+        constexpr bool next = !decltype(odd_tile)::value;
+        if (i + 1 < n) request(i + 1, Odd<next>{});
         if (i + 2 < n) look_up(i + 2);
-        compute(i);
-        if (i + 1 < n) put(i + 1);
+        compute(i, odd_tile);
+        if (i + 1 < n) put(i + 1, Odd<next>{});
+        __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
+    };
+    for (int i = 0; i < n; i += 2) {
+        step(i, Even{});
+        if (i + 1 < n) step(i + 1, Odd<true>{});
     }
 
     l += __shfl_xor(l, 32);
@@ -377,7 +431,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const 
     for (int q = 0; q < P.pieces; ++q) {
         const float *p = place + (size_t)q * ROWS * (HD + 2);
         const float2 ml = *reinterpret_cast<const float2 *>(p + (size_t)ROWS * HD + 2 * rr);
-        const float f = ml.x == -INFINITY ? 0.f : exp2f((ml.x - mx) * c2);
+        const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - mx) * c2);
         sum += f * ml.y;
         const float4 *src = reinterpret_cast<const float4 *>(p + (size_t)rr * HD + NE * part);
 #pragma unroll
