@@ -64,7 +64,13 @@ __device__ __forceinline__ Piece piece_of(const Attend &A, const SeqRows &s, int
     return p;
 }
 
-// LOADS of W bytes
+// x, hidden from what moves constant work out of loops
+__device__ __forceinline__ int anew(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// A load of W bytes
 template <int W>
 __device__ __forceinline__ uint32_t load_part(const char *p) {
     if constexpr (W == 4) return *reinterpret_cast<const uint32_t *>(p);
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     // (two variables, and the loop takes the tiles in pairs: what is on its way into one is then seen not to touch the other)
     __shared__ __align__(16) char ks_even[KT * KROW], ks_odd[KT * KROW];
     __shared__ __align__(16) char vs_even[HD * VROW], vs_odd[HD * VROW];
-    __shared__ int slots[4][KT];                  // places of the positions of four tiles, -1: not there
+    __shared__ __align__(16) long places[4][KT];  // where the positions of four tiles lie, in bytes (0 where a page is not there)
     __shared__ uint32_t there[4][2];
     __shared__ int odd[4];                        // the tile has values that are not finite where only some rows see them
 
@@ -144,54 +150,56 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     auto is_partial = [&](int key0, uint32_t th0, uint32_t th1) {
         return (th0 & th1) != 0xffffffffu || key0 + KT > full_high || (key0 < full_low && key0 + KT > sink);
     };
-    // the first wave looks up the places of the piece's tile i
-    auto look_up = [&](int i) {
-        const int u = pc.begin + i, at = i & 3;
+    // The first wave looks up the places of the piece's tile i: it asks for the page numbers a turn before it needs them
+    int page = 0;
+    auto ask = [&](int i) {
         if (wave == 0) {
-            const int j = key_of(u) + lane;
-            int slot = -1;
-            if (j < st.high) {
-                const int page = table[j / C.page_size];
-                if (page >= 0 && page < C.n_pages) slot = page * C.page_size + j % C.page_size;
-                else atomicOr(A.err_flag, ERR_PAGE);
-            }
-            slots[at][lane] = slot;
-            const unsigned long long ok = __ballot(slot >= 0);
+            const int j = key_of(pc.begin + i) + lane;
+            page = j < st.high ? table[j / C.page_size] : -1;
+        }
+    };
+    auto look_up = [&](int i) {
+        const int at = i & 3;
+        if (wave == 0) {
+            const int j = key_of(pc.begin + i) + lane;
+            const bool ok = page >= 0 && page < C.n_pages;
+            if (!ok && j < st.high) atomicOr(A.err_flag, ERR_PAGE);
+            places[at][lane] = ok ? ((long)page * C.page_size + j % C.page_size) * pitch : 0;
+            const unsigned long long all = __ballot(ok);
             if (lane == 0) {
-                there[at][0] = (uint32_t)ok;
-                there[at][1] = (uint32_t)(ok >> 32);
+                there[at][0] = (uint32_t)all;
+                there[at][1] = (uint32_t)(all >> 32);
                 odd[at] = 0;
             }
         }
     };
     uint4 kreg[KN];                               // (8 bits: keys are widened on their way; else they go to shared memory directly)
     uint32_t vreg[VK];
-    const int vd = tid % VL, vg = tid / VL;       // the thread's entries DW vd .., keys VK vg ..
+    // (a thread's values: entries DW vd .., vd = tid % VL, of keys VK vg .., vg = tid / VL)
+    // (what follows from a thread's number is worked out for each tile: kept, it would take the registers that the tile needs)
     auto request = [&](int i, auto odd_tile) {
-        const int at = i & 3;
+        const int tid = anew(threadIdx.x), lane = tid & 63, vd = tid % VL, vg = tid / VL, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even;
         if constexpr (E8) {
 #pragma unroll
             for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
-                const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP, slot = slots[at][key];
-                kreg[n] = *reinterpret_cast<const uint4 *>(kb + (slot < 0 ? 0 : slot) * pitch + 16 * part);
+                const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP;
+                kreg[n] = *reinterpret_cast<const uint4 *>(kb + 16 * part + places[at][key]);
             }
         } else {
 #pragma unroll
             for (int n = 0; n < KN; ++n) {        // 64 pieces of a wave lie side by side
                 const int first = (n * NW + wave) * 64, y = (first + lane) / KS, part = ((first + lane) % KS) ^ (y & (KS - 1));
-                const int slot = slots[at][(y & 32) + row_key(y & 31)];
-                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + (slot < 0 ? 0 : slot) * pitch + 16 * part), (las_ptr)(ks + 16 * first), 16, 0, 0);
+                const long place = places[at][(y & 32) + row_key(y & 31)];
+                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + 16 * part + place), (las_ptr)(ks + 16 * first), 16, 0, 0);
             }
         }
+        const char *const vp = vb + DW * ES * vd;
 #pragma unroll
-        for (int n = 0; n < VK; ++n) {
-            const int slot = slots[at][VK * vg + n];
-            vreg[n] = load_part<DW * ES>(vb + (slot < 0 ? 0 : slot) * pitch + DW * ES * vd);
-        }
+        for (int n = 0; n < VK; ++n) vreg[n] = load_part<DW * ES>(vp + places[at][VK * vg + n]);
     };
     auto put = [&](int i, auto odd_tile) {
-        const int u = pc.begin + i, at = i & 3;
+        const int tid = anew(threadIdx.x), vd = tid % VL, vg = tid / VL, u = pc.begin + i, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         if constexpr (E8) {
 #pragma unroll
@@ -259,7 +267,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
     auto compute = [&](int i, auto odd_tile) {
-        const int u = pc.begin + i, at = i & 3;
+        const int lane = anew(threadIdx.x) & 63, r32 = lane & 31, h = lane >> 5, u = pc.begin + i, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         const int key0 = key_of(u);
         const uint32_t th0 = there[at][0], th1 = there[at][1];
@@ -358,8 +366,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     // three tiles are on their way: the places of the one after the next, keys and values of the next, and the one at work
     const int n = pc.end - pc.begin;
     if (n > 0) {
+        ask(0);
         look_up(0);
+        ask(1);
         if (n > 1) look_up(1);
+        ask(2);
         __syncthreads();
         request(0, Even{});
         put(0, Even{});
@@ -369,7 +380,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     auto step = [&](int i, auto odd_tile) {
         constexpr bool next = !decltype(odd_tile)::value;
         if (i + 1 < n) request(i + 1, Odd<next>{});
-        if (i + 2 < n) look_up(i + 2);
+        if (i + 2 < n) {
+            look_up(i + 2);
+            if (i + 3 < n) ask(i + 3);
+        }
         compute(i, odd_tile);
         if (i + 1 < n) put(i + 1, Odd<next>{});
         __builtin_amdgcn_s_waitcnt(0x0F70);
