@@ -32,12 +32,15 @@ constexpr int STEP = 32;     // positions per step of a wave
 // head and tile of 16 RT rows, take that many units each, and the units of all items of all sequences, in order, are cut
 // into as many equal ranges as there are workgroups.  A range that ends inside an item leaves a partial result (sums, their reference m, and
 // l) in one of the workgroup's two places: place 1 if it has the item's first unit, place 0 otherwise; an item's pieces are then
-// added up in order by a second kernel.  Every kernel works the cut out anew from the lengths: nothing is planned on the host,
-// which does not know them.
+// added up in order by a second kernel.  Nothing is planned on the host, which does not know the lengths.
 struct Split {
     int rows;          // rows of a tile
-    int min_units;     // a workgroup takes at least so many
+    int tiles;         // of them that a sequence can have
     int workgroups;    // at most
+};
+// What the workgroup with an item's first unit notes of it: itself, and over how many workgroups the item goes
+struct Pieces {
+    int first, count;
 };
 
 __device__ __forceinline__ int units_of(const Attend &A, const SeqRows &s) {
@@ -47,23 +50,32 @@ __device__ __forceinline__ int units_of(const Attend &A, const SeqRows &s) {
 __device__ __forceinline__ long cost_of(const Attend &A, const Split &P, const SeqRows &s) {
     return s.n ? (long)A.cache.n_kv_heads * ((s.n * A.G + P.rows - 1) / P.rows) * units_of(A, s) : 0;
 }
-__device__ __forceinline__ long block_sum(long x, long *tmp) {   // over 256 threads
-    for (int off = 32; off > 0; off >>= 1) x += __shfl_xor(x, off);
-    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = x;
-    __syncthreads();
-    return (tmp[0] + tmp[1]) + (tmp[2] + tmp[3]);
+// x / y for 0 <= x < 2^52, 0 < y: the quotient of doubles is off by less than one
+__device__ __forceinline__ long quotient(long x, long y) {
+    long q = (long)((double)x / (double)y);
+    if (q * y > x) --q;
+    else if ((q + 1) * y <= x) ++q;
+    return q;
 }
-__device__ __forceinline__ int ranges(const Split &P, long total) {
-    const long most = total / P.min_units;
-    return most < 1 ? 1 : (most < P.workgroups ? (int)most : P.workgroups);
+// n ranges of `size` units, the first `longer` of one more
+struct Ranges {
+    int n;
+    long size, longer;
+    __device__ long begin(int w) const { return size * w + (w < longer ? w : longer); }
+};
+__device__ __forceinline__ Ranges ranges_of(const Split &P, long total) {
+    Ranges r;
+    r.n = total < 1 ? 1 : (total < P.workgroups ? (int)total : P.workgroups);
+    r.size = quotient(total, r.n);
+    r.longer = total - r.size * r.n;
+    return r;
 }
-__device__ __forceinline__ long range_begin(long total, int n, int w) { return total / n * w + total % n * w / n; }
 
 // partial results: per workgroup and place `rows` x (HD sums), then `rows` x (m, l)
 __host__ __device__ constexpr size_t place_floats(int rows, int HD) { return (size_t)rows * (HD + 2); }
 
 template <typename T, bool E8, int HD, int RT, bool AHEAD>
-__global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void paged_attention_kernel(const Attend A, const Split P, float *scratch) {
+__global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void paged_attention_kernel(const Attend A, const Split P, float *scratch, Pieces *items) {
     constexpr int ES = E8 ? 1 : 2;             // bytes of a cache entry
     constexpr int NC = HD / 32;                // contraction steps of a score
     constexpr int NE = HD / 16;                // entries of a lane's share of V, and A operands of O^T
@@ -73,13 +85,14 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
     __shared__ long scan[WAVES];
     __shared__ long seq_base;
     __shared__ int seq_at;
+    __shared__ SeqRows seq_of;
 
     const mrp_paged_cache &C = A.cache;
     const long cap = (long)C.max_pages * C.page_size;
     if (blockIdx.x == 0) check_rows(A.rows, A.n_rows, cap, A.err_flag, 64 * WAVES);
 
     // this workgroup's range, and the sequence that it begins in
-    long cur, end, base;
+    long cur, end, base, longer, size;
     int b;
     {
         const int per = (A.rows.B + 64 * WAVES - 1) / (64 * WAVES), b0 = threadIdx.x * per;
@@ -97,26 +110,32 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
             if (w < (int)(threadIdx.x >> 6)) before += scan[w];
             total += scan[w];
         }
-        const int n = ranges(P, total);
-        if ((int)blockIdx.x >= n) return;
-        cur = range_begin(total, n, blockIdx.x);
-        end = range_begin(total, n, blockIdx.x + 1);
+        const Ranges all = ranges_of(P, total);
+        if ((int)blockIdx.x >= all.n) return;
+        cur = all.begin(blockIdx.x);
+        end = all.begin(blockIdx.x + 1);
+        longer = all.longer;
+        size = all.size;
         if (cur >= end) return;
         long at = before + incl - mine;
         if (at <= cur && cur < at + mine) {
             int i = b0;
+            SeqRows s;
             for (;; ++i) {
-                const long c = cost_of(A, P, seq_rows(A.rows, A.n_rows, cap, i));
+                s = seq_rows(A.rows, A.n_rows, cap, i);
+                const long c = cost_of(A, P, s);
                 if (cur < at + c) break;
                 at += c;
             }
             seq_at = i;
             seq_base = at;
+            seq_of = s;
         }
         __syncthreads();
         b = seq_at;
         base = seq_base;
     }
+    SeqRows s = seq_of;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4, G = A.G;
     const long pitch = (long)C.n_kv_heads * HD * ES;      // bytes between positions
@@ -124,8 +143,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
     const bool causal = A.attn.causal != 0;
     const int W = A.attn.window, sink = A.attn.n_sink;
 
-    for (;; ++b) {                                        // sequences
-        const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
+    for (;; s = seq_rows(A.rows, A.n_rows, cap, ++b)) {   // sequences
         const long cost = cost_of(A, P, s);
         if (cost == 0) continue;
         const int units = units_of(A, s), nr = s.n * G, tiles = (nr + P.rows - 1) / P.rows;
@@ -134,6 +152,11 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
             const long item = (cur - base) / units;
             const int unit0 = (int)(cur - base - item * units), unit1 = units - unit0 <= end - cur ? units : unit0 + (int)(end - cur);
             const int kvh = (int)(item / tiles), row0 = (int)(item % tiles) * P.rows;
+            if (unit0 == 0 && threadIdx.x == 0) {
+                int count = 1;
+                for (long at = end, w = blockIdx.x + 1; at < cur + units; ++w, ++count) at += size + (w < longer);
+                items[((size_t)b * P.tiles + item % tiles) * C.n_kv_heads + kvh] = Pieces{(int)blockIdx.x, count};
+            }
             cur += unit1 - unit0;
             __syncthreads();                               // (the item before has been read out of shared memory)
 
@@ -446,58 +469,54 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 
 // Adds up the pieces of an item that several workgroups had a part in, in the order of its positions: 16 threads a row
 template <typename T, bool E8, int HD>
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend A, const Split P, const float *scratch) {
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend A, const Split P, const float *scratch, const Pieces *items) {
     constexpr int NE = HD / 16;
-    __shared__ long tmp[2][4];
     const mrp_paged_cache &C = A.cache;
-    const long cap = (long)C.max_pages * C.page_size;
-    const int b = blockIdx.y;
-    const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
-    const int nr = s.n * A.G, tiles = (nr + P.rows - 1) / P.rows;
-    if ((int)blockIdx.x >= tiles * C.n_kv_heads) return;
-    long total = 0, before = 0;
-    for (int i = threadIdx.x; i < A.rows.B; i += 256) {
-        const long c = cost_of(A, P, seq_rows(A.rows, A.n_rows, cap, i));
-        total += c;
-        if (i < b) before += c;
-    }
-    total = block_sum(total, tmp[0]);
-    before = block_sum(before, tmp[1]);
-    const int units = units_of(A, s), n = ranges(P, total);
-    const long i0 = before + (long)blockIdx.x * units, i1 = i0 + units;
-    // the workgroups of the item's first and last unit
-    auto owner = [&](long x) {
-        int w = (int)((double)x / (double)total * n);
-        w = w < 0 ? 0 : (w > n - 1 ? n - 1 : w);
-        while (w > 0 && range_begin(total, n, w) > x) --w;
-        while (w < n - 1 && range_begin(total, n, w + 1) <= x) ++w;
-        return w;
-    };
-    const int w0 = owner(i0), w1 = owner(i1 - 1);
-    if (w0 == w1) return;
-    const int kvh = blockIdx.x / tiles, row0 = blockIdx.x % tiles * P.rows;
+    const int b = blockIdx.y, kvh = blockIdx.x % C.n_kv_heads, tile = blockIdx.x / C.n_kv_heads;
+    const Pieces it = items[((size_t)b * P.tiles + tile) * C.n_kv_heads + kvh];   // (of no meaning where there is no such tile)
+    const SeqRows s = seq_rows(A.rows, A.n_rows, (long)C.max_pages * C.page_size, b);
+    const int nr = s.n * A.G, row0 = tile * P.rows, w0 = it.first, pieces = it.count;
+    if (row0 >= nr || pieces == 1) return;
     const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
     const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
     const size_t size = place_floats(P.rows, HD);
+    const float *const first = scratch + (2 * (size_t)w0 + 1) * size, *const others = scratch + 2 * (size_t)w0 * size;
     const int rows = nr - row0 < P.rows ? nr - row0 : P.rows, part = threadIdx.x & 15;
     for (int rr = threadIdx.x >> 4; rr < rows; rr += 16) {
+        // the row's 16 threads look at 16 pieces at a time
+        auto sums = [&](int q) {
+            return q < pieces ? *reinterpret_cast<const float2 *>((q ? others + 2 * (size_t)q * size : first) + (size_t)P.rows * HD + 2 * rr) : make_float2(-INFINITY, 0.f);
+        };
         float mx = -INFINITY, sum = 0.f, o[NE];
-        for (int w = w0; w <= w1; ++w)
-            mx = fmaxf(mx, scratch[(2 * (size_t)w + (w == w0)) * size + (size_t)P.rows * HD + 2 * rr]);
+        for (int q = part; q < pieces; q += 16) mx = fmaxf(mx, sums(q).x);
+        for (int off = 1; off < 16; off <<= 1) mx = fmaxf(mx, __shfl_xor(mx, off));
 #pragma unroll
         for (int e = 0; e < NE; ++e) o[e] = 0.f;
-        for (int w = w0; w <= w1; ++w) {
-            const float *p = scratch + (2 * (size_t)w + (w == w0)) * size;
-            const float2 ml = *reinterpret_cast<const float2 *>(p + (size_t)P.rows * HD + 2 * rr);
-            const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - mx) * c2);
-            sum += f * ml.y;
-            const float4 *src = reinterpret_cast<const float4 *>(p + (size_t)rr * HD + NE * part);
+        for (int q0 = 0; q0 < pieces; q0 += 16) {
+            const float2 ml = sums(q0 + part);
+            const float mine = ml.x == -INFINITY ? 0.f : exp2_((ml.x - mx) * c2);
+            sum += mine * ml.y;
+            const int count = pieces - q0 < 16 ? pieces - q0 : 16;
+            for (int q1 = 0; q1 < count; q1 += 4) {      // (four requests at a time; past the end the last piece again, at a weight of zero)
+                float4 v[4][NE / 4];
 #pragma unroll
-            for (int e = 0; e < NE; e += 4) {
-                const float4 v = src[e / 4];
-                o[e] += f * v.x; o[e + 1] += f * v.y; o[e + 2] += f * v.z; o[e + 3] += f * v.w;
+                for (int x = 0; x < 4; ++x) {
+                    const int q = q0 + (q1 + x < count ? q1 + x : count - 1);
+                    const float4 *src = reinterpret_cast<const float4 *>((q ? others + 2 * (size_t)q * size : first) + (size_t)rr * HD + NE * part);
+#pragma unroll
+                    for (int e = 0; e < NE / 4; ++e) v[x][e] = src[e];
+                }
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const float f = q1 + x < count ? __shfl(mine, (threadIdx.x & 48) + q1 + x) : 0.f;
+#pragma unroll
+                    for (int e = 0; e < NE; e += 4) {
+                        o[e] += f * v[x][e / 4].x; o[e + 1] += f * v[x][e / 4].y; o[e + 2] += f * v[x][e / 4].z; o[e + 3] += f * v[x][e / 4].w;
+                    }
+                }
             }
         }
+        for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor(sum, off);
         const int r = row0 + rr, t = r / A.G;
         store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
     }
@@ -505,23 +524,20 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend 
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
-// Rows of a tile: the fewest that hold a sequence's rows, up to 64 (32 of 256 entries: registers)
-int tile_rows(long rows, int HD) { return rows <= 16 ? 16 : (rows <= 32 || HD == 256 ? 32 : 64); }
-
-// The largest number of workgroups is what fits the device at once: two a compute unit for 16 rows of up to 128 entries, else one
+// Rows of a tile: the fewest that hold a sequence's rows, up to 32.  The largest number of workgroups is what fits the device at
+// once: two a compute unit for 16 rows of up to 128 entries, else one
 Split split_of(long rows, int HD, int nCU) {
-    const int tr = tile_rows(rows, HD);
-    return Split{tr, 1, (tr == 16 && HD <= 128 ? 2 : 1) * (nCU > 0 ? nCU : 1)};
+    const int tr = rows <= 16 ? 16 : 32;
+    return Split{tr, ceil_div(rows, tr), (tr == 16 && HD <= 128 ? 2 : 1) * (nCU > 0 ? nCU : 1)};
 }
+size_t partial_floats(const Split &p, int HD) { return 2 * (size_t)p.workgroups * place_floats(p.rows, HD); }
 
 template <typename T, bool E8, int HD>
 void launch(const Attend &a, const Split &p, float *scratch, hipStream_t st) {
-    constexpr bool AH = false;
-    if (p.rows == 16) paged_attention_kernel<T, E8, HD, 1, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
-    else if (p.rows == 32) paged_attention_kernel<T, E8, HD, 2, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
-    else if constexpr (HD < 256) paged_attention_kernel<T, E8, HD, 4, AH><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch);
-    const int tiles = ceil_div(most_rows(a.n_rows, a.rows, a.G), p.rows);
-    paged_attention_join_kernel<T, E8, HD><<<dim3(tiles * a.cache.n_kv_heads, a.rows.B), 256, 0, st>>>(a, p, scratch);
+    Pieces *const items = reinterpret_cast<Pieces *>(scratch + partial_floats(p, HD));
+    if (p.rows == 16) paged_attention_kernel<T, E8, HD, 1, false><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
+    else paged_attention_kernel<T, E8, HD, 2, false><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
+    paged_attention_join_kernel<T, E8, HD><<<dim3(p.tiles * a.cache.n_kv_heads, a.rows.B), 256, 0, st>>>(a, p, scratch, items);
 }
 
 template <typename T, bool E8>
@@ -556,7 +572,7 @@ size_t mrp_paged_attention_scratch_bytes(const mrp_ctx *c, long n_rows, const mr
         return prompt_scratch_floats(per_head, rows->B, cache->n_kv_heads, (long)cache->max_pages * cache->page_size, cache->head_dim,
                                      ctx_view(c).nCU) * sizeof(float);
     const Split p = split_of(per_head, cache->head_dim, ctx_view(c).nCU);
-    return 2 * (size_t)p.workgroups * place_floats(p.rows, cache->head_dim) * sizeof(float);
+    return partial_floats(p, cache->head_dim) * sizeof(float) + (size_t)rows->B * p.tiles * cache->n_kv_heads * sizeof(Pieces);
 }
 
 int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_rows *rows, const mrp_paged_cache *cache,

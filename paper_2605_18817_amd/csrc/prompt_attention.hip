@@ -89,9 +89,11 @@ __device__ __forceinline__ void four_ahead() {
     __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
 }
 
-template <typename T, bool E8, int HD, int NW>
+// NW waves; KH: the keys of a tile are halved between two waves with the same rows (2) or not (1)
+template <typename T, bool E8, int HD, int NW, int KH>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Attend A, const Cut P, float *scratch) {
-    constexpr int ES = E8 ? 1 : 2, THREADS = 64 * NW, ROWS = 32 * NW;
+    constexpr int ES = E8 ? 1 : 2, THREADS = 64 * NW, ROWS = 32 * NW / KH;
+    constexpr int NT = 2 / KH;                    // halves of a tile that a wave takes
     constexpr int NC = HD / 16;                   // contraction steps of a score
     constexpr int ND = HD / 32;                   // tiles of 32 entries of the output
     constexpr int KROW = HD * 2;                  // bytes of a key's row in shared memory: piece x of row y lies in place x ^ y % KS,
@@ -124,9 +126,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     const Piece pc = piece_of(A, s, row0, ROWS, nr, P.pieces, piece);
     const Steps &st = pc.st;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, h = lane >> 5;
+    const int part = wave % (NW / KH), half = wave / (NW / KH);   // of the rows, and of a tile's keys
 
     // the row's position and operand (lanes past the last row take it again and store nothing)
-    const int my = row0 + 32 * wave + r32, r = my < nr ? my : nr - 1;
+    const int my = row0 + 32 * part + r32, r = my < nr ? my : nr - 1;
     const int tok = r / G, pos = s.len - s.n + tok, head = kvh * G + r - tok * G;
     u32x4 qf[NC];
     {
@@ -271,30 +274,32 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         const int key0 = key_of(u);
         const uint32_t th0 = there[at][0], th1 = there[at][1];
-        f32x16 sc[2];
+        f32x16 sc[NT];
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < NT; ++t) {
+            const int half_key = 32 * (KH == 2 ? half : t);
 #pragma unroll
             for (int i = 0; i < 16; ++i) sc[t][i] = 0.f;
 #pragma unroll
             for (int c = 0; c < NC; ++c) {
-                const u32x4 a = *reinterpret_cast<const u32x4 *>(ks + (32 * t + r32) * KROW + ((32 * c) ^ (16 * (h ^ (r32 & (KS - 1))))));
+                const u32x4 a = *reinterpret_cast<const u32x4 *>(ks + (half_key + r32) * KROW + ((32 * c) ^ (16 * (h ^ (r32 & (KS - 1))))));
                 sc[t] = mfma32(T{}, a, qf[c], sc[t]);
             }
         }
-        four_ahead<2 * NC>();
+        four_ahead<NT * NC>();
         const bool partial = is_partial(key0, th0, th1);
         if (partial) {
 #pragma unroll
-            for (int t = 0; t < 2; ++t) {
-                const uint32_t seen = (seen_bits(pos, key0 + 32 * t, s.len, A.attn) & (t ? th1 : th0)) >> (8 * h);
+            for (int t = 0; t < NT; ++t) {
+                const int tt = KH == 2 ? half : t;
+                const uint32_t seen = (seen_bits(pos, key0 + 32 * tt, s.len, A.attn) & (tt ? th1 : th0)) >> (8 * h);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[t][i] = (seen >> (16 * (i >> 3) + (i & 7))) & 1u ? sc[t][i] : -INFINITY;
             }
         }
         float mx = sc[0][0];
 #pragma unroll
-        for (int i = 1; i < 32; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+        for (int i = 1; i < 16 * NT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         // the sums are brought to a new reference where a score is more than a factor of 2^8 above the old one
         if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx > m))) {
@@ -306,10 +311,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             for (int d = 0; d < ND; ++d) acc[d] *= alpha;
         }
         const float ref = m == -INFINITY ? 0.f : m * c2;
-        u32x4 p[4];                               // the weights of 16 keys each, rounded to 16 bits
+        u32x4 p[2 * NT];                          // the weights of 16 keys each, rounded to 16 bits
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 32; i += 2) {
+        for (int i = 0; i < 16 * NT; i += 2) {
             const float p0 = exp2_(fmaf(sc[i >> 4][i & 15], c2, -ref)), p1 = exp2_(fmaf(sc[i >> 4][(i & 15) + 1], c2, -ref));
             float x, y;
             sum += p0 + p1;
@@ -319,10 +324,10 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         if (partial && odd[at]) {
             // A weight of zero times a value that is not finite is not zero.  Such values leave the product; how many of them a row
             // sees in an entry is a product too, of ones, and makes the row's entry NaN
-            u32x4 sees[4];
+            u32x4 sees[2 * NT];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t seen = seen_bits(pos, key0 + 32 * (q >> 1), s.len, A.attn) >> (16 * (q & 1) + 8 * h);
+            for (int q = 0; q < 2 * NT; ++q) {
+                const uint32_t seen = seen_bits(pos, key0 + 32 * (KH == 2 ? half : q >> 1), s.len, A.attn) >> (16 * (q & 1) + 8 * h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) sees[q][j] = ((seen >> (2 * j)) & 1u) * one_bits(T{}) + (((seen >> (2 * j + 1)) & 1u) * one_bits(T{}) << 16);
             }
@@ -332,8 +337,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
                 for (int i = 0; i < 16; ++i) count[i] = 0.f;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 16 * h);
+                for (int q = 0; q < 2 * NT; ++q) {
+                    u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 64 * (KH == 2 ? half : 0) + 16 * h);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) a[j] = odd_halves(T{}, a[j]);
                     count = mfma32(T{}, a, sees[q], count);
@@ -356,11 +361,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 16 * h);
+            for (int q = 0; q < 2 * NT; ++q) {
+                const u32x4 a = *reinterpret_cast<const u32x4 *>(vs + (32 * d + r32) * VROW + 32 * q + 64 * (KH == 2 ? half : 0) + 16 * h);
                 acc[d] = mfma32(T{}, a, p[q], acc[d]);
             }
-        four_ahead<4 * ND>();
+        four_ahead<2 * NT * ND>();
     };
 
     // three tiles are on their way: the places of the one after the next, keys and values of the next, and the one at work
@@ -395,12 +400,33 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     }
 
     l += __shfl_xor(l, 32);
+    if constexpr (KH == 2) {                      // the two waves of a row add up (the tiles' places are free)
+        float *const mine = reinterpret_cast<float *>(part ? vs_odd : vs_even) + lane;
+        if (half == 1) {
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mine[(16 * d + i) * 64] = acc[d][i];
+            mine[16 * ND * 64] = m;
+            mine[(16 * ND + 1) * 64] = l;
+        }
+        __syncthreads();
+        if (half == 1) return;
+        const float m1 = mine[16 * ND * 64], l1 = mine[(16 * ND + 1) * 64], top = fmaxf(m, m1);
+        const float f0 = m == -INFINITY ? 0.f : exp2_((m - top) * c2), f1 = m1 == -INFINITY ? 0.f : exp2_((m1 - top) * c2);
+        m = top;
+        l = l * f0 + l1 * f1;
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * f0 + mine[(16 * d + i) * 64] * f1;
+    }
     if (my >= nr) return;
     const bool empty = m == -INFINITY;
     const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
     if (P.pieces > 1) {
         float *place = scratch + (((size_t)b * P.tiles + tile) * C.n_kv_heads + kvh) * P.pieces * ROWS * (HD + 2) + (size_t)piece * ROWS * (HD + 2);
-        float *dst = place + (size_t)(32 * wave + r32) * HD;
+        float *dst = place + (size_t)(32 * part + r32) * HD;
 #pragma unroll
         for (int d = 0; d < ND / 2; ++d)
 #pragma unroll
@@ -409,7 +435,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
                 to[0] = make_float4(acc[d][i], acc[d + ND / 2][i], acc[d][i + 1], acc[d + ND / 2][i + 1]);
                 to[1] = make_float4(acc[d][i + 2], acc[d + ND / 2][i + 2], acc[d][i + 3], acc[d + ND / 2][i + 3]);
             }
-        if (h == 0) *reinterpret_cast<float2 *>(place + (size_t)ROWS * HD + 2 * (32 * wave + r32)) = make_float2(m, l);
+        if (h == 0) *reinterpret_cast<float2 *>(place + (size_t)ROWS * HD + 2 * (32 * part + r32)) = make_float2(m, l);
         return;
     }
     const long at = (long)(s.begin + tok) * A.attn.n_heads + head;
@@ -428,9 +454,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 }
 
 // Adds up a row tile's pieces in the order of their positions: 16 threads a row, 16 rows a workgroup
-template <typename T, bool E8, int HD, int NW>
+template <typename T, bool E8, int HD, int ROWS>
 __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const Cut P, const float *scratch) {
-    constexpr int ROWS = 32 * NW, NE = HD / 16;
+    constexpr int NE = HD / 16;
     const mrp_paged_cache &C = A.cache;
     const int per = ROWS / 16, b = blockIdx.y, slice = blockIdx.x % per, kvh = blockIdx.x / per % C.n_kv_heads, tile = blockIdx.x / per / C.n_kv_heads;
     const SeqRows s = seq_rows(A.rows, A.n_rows, (long)C.max_pages * C.page_size, b);
@@ -458,49 +484,59 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const 
     store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, sum, E8 && C.v_scale ? C.v_scale[kvh] : 1.f, o);
 }
 
-// Waves of a workgroup: four where a sequence has no more than 128 rows of a key head
-int waves_for(long rows) { return rows <= 128 ? 4 : 8; }
+// Rows of a workgroup: 64 (four waves, keys halved between them), 128 (four waves) or 256 (eight)
+int tile_rows(long rows) { return rows <= 64 ? 64 : (rows <= 128 ? 128 : 256); }
 
-// Pieces: as many as find a compute unit each, while a piece keeps four tiles of the longest sequence that the table allows
+// Pieces: as many as find a place on the device (two workgroups of four waves on a compute unit, one of eight), while a piece keeps
+// four tiles of the longest sequence that the table allows.  Twice as many for up to 64 rows, whose time is that of the
+// longest sequence.
 Cut cut_of(long rows, int B, int n_kv_heads, long positions, int nCU) {
     Cut c;
-    const int per = 32 * waves_for(rows);
+    const int per = tile_rows(rows);
     c.tiles = (int)((rows + per - 1) / per);
     const long items = (long)c.tiles * B * n_kv_heads, longest = positions / (4 * KT);
-    long pieces = items > 0 ? nCU / items : 1;
+    long pieces = items > 0 ? (per == 64 ? 4 : (per == 128 ? 2 : 1)) * (long)nCU / items : 1;
     if (pieces > longest) pieces = longest;
     c.pieces = pieces < 1 ? 1 : (int)pieces;
     return c;
 }
 
-template <typename T, bool E8, int HD, int NW>
+template <typename T, bool E8, int HD, int NW, int KH>
 void launch(const Attend &a, const Cut &c, float *scratch, hipStream_t st) {
-    prompt_attention_kernel<T, E8, HD, NW><<<dim3(c.tiles * a.cache.n_kv_heads * c.pieces, a.rows.B), 64 * NW, 0, st>>>(a, c, scratch);
+    constexpr int ROWS = 32 * NW / KH;
+    prompt_attention_kernel<T, E8, HD, NW, KH><<<dim3(c.tiles * a.cache.n_kv_heads * c.pieces, a.rows.B), 64 * NW, 0, st>>>(a, c, scratch);
     if (c.pieces > 1)
-        prompt_join_kernel<T, E8, HD, NW><<<dim3(c.tiles * a.cache.n_kv_heads * (2 * NW), a.rows.B), 256, 0, st>>>(a, c, scratch);
+        prompt_join_kernel<T, E8, HD, ROWS><<<dim3(c.tiles * a.cache.n_kv_heads * (ROWS / 16), a.rows.B), 256, 0, st>>>(a, c, scratch);
 }
 
+template <typename T, bool E8, int HD>
+void launch_form(const Attend &a, const Cut &c, int rows, float *scratch, hipStream_t st) {
+    if (rows == 64) launch<T, E8, HD, 4, 2>(a, c, scratch, st);
+    else if (rows == 128) launch<T, E8, HD, 4, 1>(a, c, scratch, st);
+    else launch<T, E8, HD, 8, 1>(a, c, scratch, st);
+}
 template <typename T, bool E8>
-void launch_form(const Attend &a, const Cut &c, int waves, float *scratch, hipStream_t st) {
-    if (a.cache.head_dim == 64) waves == 4 ? launch<T, E8, 64, 4>(a, c, scratch, st) : launch<T, E8, 64, 8>(a, c, scratch, st);
-    else waves == 4 ? launch<T, E8, 128, 4>(a, c, scratch, st) : launch<T, E8, 128, 8>(a, c, scratch, st);
+void launch_hd(const Attend &a, const Cut &c, int rows, float *scratch, hipStream_t st) {
+    if (a.cache.head_dim == 64) launch_form<T, E8, 64>(a, c, rows, scratch, st);
+    else launch_form<T, E8, 128>(a, c, rows, scratch, st);
 }
 
 }  // namespace
 
-bool prompt_takes(long rows, int head_dim) { return rows > 64 && head_dim <= 128; }
+bool prompt_takes(long rows, int head_dim) { return rows > 32 && head_dim <= 128; }
 
 size_t prompt_scratch_floats(long rows, int B, int n_kv_heads, long positions, int head_dim, int nCU) {
     const Cut c = cut_of(rows, B, n_kv_heads, positions, nCU);
-    return c.pieces > 1 ? (size_t)c.tiles * B * n_kv_heads * c.pieces * 32 * waves_for(rows) * (head_dim + 2) : 0;
+    return c.pieces > 1 ? (size_t)c.tiles * B * n_kv_heads * c.pieces * tile_rows(rows) * (head_dim + 2) : 0;
 }
 
 hipError_t launch_prompt_attention(const Attend &a, float *scratch, int nCU, hipStream_t st) {
     const long rows = most_rows(a.n_rows, a.rows, a.G);
     const Cut c = cut_of(rows, a.rows.B, a.cache.n_kv_heads, (long)a.cache.max_pages * a.cache.page_size, nCU);
     const bool e8 = a.cache.dtype == MRP_DTYPE_E4M3;
-    if (a.attn.dtype == MRP_DTYPE_BF16) e8 ? launch_form<BF16, true>(a, c, waves_for(rows), scratch, st) : launch_form<BF16, false>(a, c, waves_for(rows), scratch, st);
-    else e8 ? launch_form<F16, true>(a, c, waves_for(rows), scratch, st) : launch_form<F16, false>(a, c, waves_for(rows), scratch, st);
+    const int per = tile_rows(rows);
+    if (a.attn.dtype == MRP_DTYPE_BF16) e8 ? launch_hd<BF16, true>(a, c, per, scratch, st) : launch_hd<BF16, false>(a, c, per, scratch, st);
+    else e8 ? launch_hd<F16, true>(a, c, per, scratch, st) : launch_hd<F16, false>(a, c, per, scratch, st);
     return hipGetLastError();
 }
 
