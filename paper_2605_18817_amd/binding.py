@@ -160,42 +160,69 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-_DTYPES = {"torch.float32": 0, "torch.bfloat16": 1, "torch.float16": 2, "torch.float8_e4m3fn": 3}
+_DTYPES: dict = {}          # torch.dtype -> MRP_DTYPE_*, filled on first use
 
 
-def _dtype(t, allowed: str) -> int:
-    code = _DTYPES.get(str(t.dtype), -1)
-    if code < 0 or str(code) not in allowed:
+def _dtypes() -> dict:
+    if not _DTYPES:
+        import torch
+        _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2, torch.float8_e4m3fn: 3, torch.int32: -32})
+    return _DTYPES
+
+
+def _dtype(t, allowed) -> int:
+    code = _dtypes().get(t.dtype)
+    if code is None or code not in allowed:
         raise MrpError(f"no form for tensors of {t.dtype} here")
     return code
 
 
-def _plain(t, name: str, dtypes: str, shape) -> Optional[int]:
-    """Address of a dense device tensor of one of the types and of this shape (None stays NULL)."""
+_FLOATS, _HALVES, _CACHES, _INT = (0, 1, 2), (1, 2), (1, 2, 3), -32
+
+
+def _dense(t, name: str, dtype: int, shape, device: int) -> Optional[int]:
+    """Address of a dense tensor of this type and shape on the device (None stays NULL)."""
     if t is None:
         return None
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise MrpError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if dtypes == "i":
-        if str(t.dtype) != "torch.int32":
-            raise MrpError(f"{name}: {t.dtype}, expected int32")
-    else:
-        _dtype(t, dtypes)
-    return _ptr(t)
+    if _DTYPES.get(t.dtype) != dtype:
+        raise MrpError(f"{name}: {t.dtype} does not fit here")
+    if t.get_device() != device or not t.is_contiguous():
+        raise MrpError(f"{name}: a contiguous tensor on device {device} is needed")
+    return t.data_ptr()
 
 
-def _row_tensor(t, name: str, heads: int, head_dim: int, n_rows: int, dtype: int):
-    """(address, row stride) of a device tensor [n_rows][heads][head_dim] whose rows are dense in themselves."""
+def _rows(t, name: str, shape, dtype: int, device: int):
+    """(address, row stride) of a tensor [n_rows][heads][head_dim] on the device whose rows are dense in themselves."""
     if t is None:
         return None, 0
-    if tuple(t.shape) != (n_rows, heads, head_dim):
-        raise MrpError(f"{name}: shape {tuple(t.shape)}, expected {(n_rows, heads, head_dim)}")
-    if _DTYPES.get(str(t.dtype), -1) != dtype:
+    if t.shape != shape:
+        raise MrpError(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if _DTYPES.get(t.dtype) != dtype:
         raise MrpError(f"{name}: {t.dtype} is not the type that the others have")
-    st = t.stride()
-    if not t.is_cuda or st[2] != 1 or (heads > 1 and st[1] != head_dim):
-        raise MrpError(f"{name}: a device tensor whose heads lie side by side is needed")
-    return t.data_ptr(), (st[0] if n_rows > 1 else heads * head_dim)
+    row, head, one = t.stride()
+    n, heads, head_dim = shape
+    if t.get_device() != device or one != 1 or (heads > 1 and head != head_dim):
+        raise MrpError(f"{name}: a tensor on device {device} whose heads lie side by side is needed")
+    return t.data_ptr(), (row if n > 1 else heads * head_dim)
+
+
+def _device_of(*tensors) -> Optional[int]:
+    """The one device that the tensors (None: not given) are on."""
+    found = {t.get_device() for t in tensors if t is not None}
+    if len(found) > 1 or -1 in found:
+        raise MrpError("tensors on one GPU are needed")
+    return found.pop() if found else None
+
+
+def _scratch(t, device: int):
+    """(address, bytes) of a caller's scratch tensor."""
+    if t is None:
+        return None, 0
+    if t.get_device() != device or not t.is_contiguous():
+        raise MrpError(f"scratch: a contiguous tensor on device {device} is needed")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _stream() -> int:
@@ -273,22 +300,26 @@ class QkNormRope:
     def __init__(self, n_heads: int, n_kv_heads: int, head_dim: int, rope=None, q_gain=None, k_gain=None,
                  eps: float = 1e-6):
         gain = q_gain if q_gain is not None else k_gain
-        if q_gain is not None and k_gain is not None and q_gain.dtype != k_gain.dtype:
-            raise MrpError("gains of two types")
+        gain_dtype = 1 if gain is None else _dtype(gain, _FLOATS)
         rot, n_pos = 0, 0
         if rope is not None:
             n_pos, rot = rope.shape[0], 2 * rope.shape[1]
+        _dtypes()
         self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim = n_heads, n_kv_heads, head_dim, rot
         self.tensors = (rope, q_gain, k_gain)
-        self.c = _Qk(n_heads, n_kv_heads, head_dim, rot, 0, 0, 1 if gain is None else _dtype(gain, "012"), eps,
-                     _plain(q_gain, "q_gain", "012", (head_dim,)), _plain(k_gain, "k_gain", "012", (head_dim,)),
-                     _plain(rope, "rope", "0", (n_pos, rot // 2, 2)), n_pos)
+        self.device = dev = _device_of(*self.tensors)
+        self._args = (gain_dtype, eps, _dense(q_gain, "q_gain", gain_dtype, (head_dim,), dev),
+                      _dense(k_gain, "k_gain", gain_dtype, (head_dim,), dev),
+                      _dense(rope, "rope", 0, (n_pos, rot // 2, 2), dev), n_pos)
+        self._typed: dict = {}
 
-    def typed(self, x_dtype: int, y_dtype: int) -> _Qk:
-        c = _Qk()
-        C.memmove(C.byref(c), C.byref(self.c), C.sizeof(_Qk))
-        c.x_dtype, c.y_dtype = x_dtype, y_dtype
-        return c
+    def typed(self, x_dtype: int, y_dtype: int):
+        """The description for inputs and outputs of these types, as a call takes it."""
+        ref = self._typed.get((x_dtype, y_dtype))
+        if ref is None:
+            c = _Qk(self.n_heads, self.n_kv_heads, self.head_dim, self.rotary_dim, x_dtype, y_dtype, *self._args)
+            ref = self._typed[(x_dtype, y_dtype)] = C.byref(c)
+        return ref
 
 
 class NewRows:
@@ -296,10 +327,13 @@ class NewRows:
     sequence, ``cu_rows`` int32 [B + 1] or None where every sequence has max_new."""
 
     def __init__(self, kv_len, max_new: int, cu_rows=None):
-        self.B = kv_len.shape[0]
+        _dtypes()
+        self.B = B = kv_len.shape[0]
         self.tensors = (kv_len, cu_rows)
-        self.c = _NewRows(self.B, max_new, _plain(cu_rows, "cu_rows", "i", (self.B + 1,)),
-                          _plain(kv_len, "kv_len", "i", (self.B,)))
+        self.device = dev = _device_of(*self.tensors)
+        self.shape = (B, max_new)
+        self.ref = C.byref(_NewRows(B, max_new, _dense(cu_rows, "cu_rows", _INT, (B + 1,), dev),
+                                    _dense(kv_len, "kv_len", _INT, (B,), dev)))
 
 
 class PagedCache:
@@ -307,14 +341,17 @@ class PagedCache:
     fp16 or float8_e4m3fn, page_table int32 [B][max_pages], scales fp32 [n_kv_heads] for 8 bits."""
 
     def __init__(self, k_pages, v_pages, page_table, k_scale=None, v_scale=None):
-        if k_pages.dim() != 4 or v_pages.dtype != k_pages.dtype or page_table.dim() != 2:
-            raise MrpError("pages [n_pages][page_size][n_kv_heads][head_dim] of one type and a table [B][max_pages] are needed")
+        if k_pages.dim() != 4 or page_table.dim() != 2:
+            raise MrpError("pages [n_pages][page_size][n_kv_heads][head_dim] and a table [B][max_pages] are needed")
         n, ps, hkv, hd = k_pages.shape
-        self.B, self.n_kv_heads, self.head_dim, self.dtype = page_table.shape[0], hkv, hd, _dtype(k_pages, "123")
+        self.B, self.n_kv_heads, self.head_dim, self.dtype = page_table.shape[0], hkv, hd, _dtype(k_pages, _CACHES)
         self.tensors = (k_pages, v_pages, page_table, k_scale, v_scale)
-        self.c = _PagedCache(_ptr(k_pages), _plain(v_pages, "v_pages", "123", k_pages.shape), self.dtype, hkv, hd, n, ps,
-                             _plain(page_table, "page_table", "i", page_table.shape), page_table.shape[1],
-                             _plain(k_scale, "k_scale", "0", (hkv,)), _plain(v_scale, "v_scale", "0", (hkv,)))
+        self.device = dev = _device_of(*self.tensors)
+        self.shape = (self.B, hkv, hd, ps * page_table.shape[1])
+        self.ref = C.byref(_PagedCache(
+            _dense(k_pages, "k_pages", self.dtype, k_pages.shape, dev), _dense(v_pages, "v_pages", self.dtype, k_pages.shape, dev),
+            self.dtype, hkv, hd, n, ps, _dense(page_table, "page_table", _INT, page_table.shape, dev), page_table.shape[1],
+            _dense(k_scale, "k_scale", 0, (hkv,), dev), _dense(v_scale, "v_scale", 0, (hkv,), dev)))
 
 
 @dataclass
@@ -369,6 +406,8 @@ class MrpContext:
             raise MrpError(f"mrp_create failed: {rc}")
         self._h = h
         self.device = torch.cuda.current_device()
+        self._get_stream = torch._C._cuda_getCurrentRawStream
+        self._scratch_bytes: dict = {}
 
     def close(self):
         if getattr(self, "_h", None):
@@ -506,99 +545,100 @@ class MrpContext:
                                        _ptr(rms_pair), _ptr(rms_delta))
         return self._check(rc, "mrp_residual_rms") if check else rc
 
-    def _here(self, *tensors):
-        """The tensors are on the context's device (the call itself refuses another current device)."""
-        for t in tensors:
-            if t is not None and t.get_device() != self.device:
-                raise MrpError(f"a tensor on {t.device}: the context is of device {self.device}")
+    def _here(self, *things):
+        """The descriptions are of the context's device (the call itself refuses another current device)."""
+        for x in things:
+            if x.device is not None and x.device != self.device:
+                raise MrpError(f"tensors on device {x.device}: the context is of device {self.device}")
+
+    def _raw_stream(self) -> int:
+        """The current stream of the context's device (the same as _stream() where that device is the current one)."""
+        return self._get_stream(self.device)
 
     def rope_table(self, n_pos: int, rotary_dim: int, theta: float):
         """cos and sin of every position and pair: fp32 [n_pos][rotary_dim / 2][2]."""
         import torch
         out = torch.empty((n_pos, rotary_dim // 2, 2), dtype=torch.float32, device=f"cuda:{self.device}")
-        self._check(self.lib.mrp_rope_table(self._h, _stream(), n_pos, rotary_dim, theta, _ptr(out)), "mrp_rope_table")
+        self._check(self.lib.mrp_rope_table(self._h, self._raw_stream(), n_pos, rotary_dim, theta, out.data_ptr()), "mrp_rope_table")
         return out
 
     def qk_norm_rope(self, qk: QkNormRope, pos, q, k, q_out, k_out, check: bool = True) -> int:
         """q [n][n_heads][head_dim], k [n][n_kv_heads][head_dim] -> q_out, k_out; pos int32 [n]."""
-        n = q.shape[0]
-        self._here(pos, q, k, q_out, k_out, *qk.tensors)
-        x, y = _dtype(q, "012"), _dtype(q_out, "012")
-        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
-        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
-        rc = self.lib.mrp_qk_norm_rope(self._h, _stream(), n, C.byref(qk.typed(x, y)), _plain(pos, "pos", "i", (n,)), qp, qs,
-                                       kp, ks, _plain(q_out, "q_out", str(y), (n, qk.n_heads, qk.head_dim)),
-                                       _plain(k_out, "k_out", str(y), (n, qk.n_kv_heads, qk.head_dim)))
+        self._here(qk)
+        dev, n, hd = self.device, q.shape[0], qk.head_dim
+        x, y = _dtype(q, _FLOATS), _dtype(q_out, _FLOATS)
+        qs, ks = (n, qk.n_heads, hd), (n, qk.n_kv_heads, hd)
+        rc = self.lib.mrp_qk_norm_rope(self._h, self._raw_stream(), n, qk.typed(x, y), _dense(pos, "pos", _INT, (n,), dev),
+                                       *_rows(q, "q", qs, x, dev), *_rows(k, "k", ks, x, dev),
+                                       _dense(q_out, "q_out", y, qs, dev), _dense(k_out, "k_out", y, ks, dev))
         return self._check(rc, "mrp_qk_norm_rope") if check else rc
 
     def qk_norm_rope_grad(self, qk: QkNormRope, pos, q, k, dq_out, dk_out, dq, dk, dq_gain=None, dk_gain=None, scratch=None,
                           check: bool = True) -> int:
         """Gradients of qk_norm_rope: dq, dk (like q, k) and the gains' (fp32 [head_dim]) from dq_out, dk_out.  scratch: a
         uint8 tensor of qk_norm_rope_grad_scratch_bytes, or None to take one from torch's allocator."""
-        import torch
-        n = q.shape[0]
-        self._here(pos, q, k, dq_out, dk_out, dq, dk, dq_gain, dk_gain, scratch, *qk.tensors)
-        x, y = _dtype(q, "012"), _dtype(dq_out, "012")
-        c = qk.typed(x, y)
-        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
-        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
-        dqp, dqs = _row_tensor(dq, "dq", qk.n_heads, qk.head_dim, n, x)
-        dkp, dks = _row_tensor(dk, "dk", qk.n_kv_heads, qk.head_dim, n, x)
+        self._here(qk)
+        dev, n, hd = self.device, q.shape[0], qk.head_dim
+        x, y = _dtype(q, _FLOATS), _dtype(dq_out, _FLOATS)
+        qs, ks, ref = (n, qk.n_heads, hd), (n, qk.n_kv_heads, hd), qk.typed(x, y)
         if scratch is None:
-            scratch = torch.empty(self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, C.byref(c)), dtype=torch.uint8, device=q.device)
-        rc = self.lib.mrp_qk_norm_rope_grad(self._h, _stream(), n, C.byref(c), _plain(pos, "pos", "i", (n,)), qp, qs, kp, ks,
-                                            _plain(dq_out, "dq_out", str(y), (n, qk.n_heads, qk.head_dim)),
-                                            _plain(dk_out, "dk_out", str(y), (n, qk.n_kv_heads, qk.head_dim)), dqp, dqs, dkp, dks,
-                                            _plain(dq_gain, "dq_gain", "0", (qk.head_dim,)),
-                                            _plain(dk_gain, "dk_gain", "0", (qk.head_dim,)), _ptr(scratch),
-                                            scratch.numel() * scratch.element_size())
+            import torch
+            scratch = torch.empty(self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, ref), dtype=torch.uint8, device=q.device)
+        rc = self.lib.mrp_qk_norm_rope_grad(self._h, self._raw_stream(), n, ref, _dense(pos, "pos", _INT, (n,), dev),
+                                            *_rows(q, "q", qs, x, dev), *_rows(k, "k", ks, x, dev),
+                                            _dense(dq_out, "dq_out", y, qs, dev), _dense(dk_out, "dk_out", y, ks, dev),
+                                            *_rows(dq, "dq", qs, x, dev), *_rows(dk, "dk", ks, x, dev),
+                                            _dense(dq_gain, "dq_gain", 0, (hd,), dev), _dense(dk_gain, "dk_gain", 0, (hd,), dev),
+                                            *_scratch(scratch, dev))
         return self._check(rc, "mrp_qk_norm_rope_grad") if check else rc
 
     def qk_norm_rope_grad_scratch_bytes(self, qk: QkNormRope, n: int) -> int:
-        return self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, C.byref(qk.c))
+        return self.lib.mrp_qk_norm_rope_grad_scratch_bytes(n, qk.typed(1, 1))
 
     def cache_append(self, rows: NewRows, qk: QkNormRope, q, k, v, cache: PagedCache, q_out, check: bool = True) -> int:
         """Norm, rotate and append k, append v, and norm and rotate q into q_out (q and q_out None: keys and values only)."""
-        n = k.shape[0]
-        self._here(q, k, v, q_out, *rows.tensors, *qk.tensors, *cache.tensors)
+        self._here(rows, qk, cache)
         if rows.B != cache.B:
             raise MrpError(f"{rows.B} sequences, but a page table of {cache.B}")
         if (q is None) != (q_out is None):
             raise MrpError("q and q_out go together")
-        x = _dtype(k, "012")
-        y = x if q_out is None else _dtype(q_out, "012")
-        qp, qs = _row_tensor(q, "q", qk.n_heads, qk.head_dim, n, x)
-        kp, ks = _row_tensor(k, "k", qk.n_kv_heads, qk.head_dim, n, x)
-        vp, vs = _row_tensor(v, "v", qk.n_kv_heads, qk.head_dim, n, x)
-        rc = self.lib.mrp_cache_append(self._h, _stream(), n, C.byref(rows.c), C.byref(qk.typed(x, y)), qp, qs, kp, ks, vp, vs,
-                                       C.byref(cache.c), _plain(q_out, "q_out", str(y), (n, qk.n_heads, qk.head_dim)))
+        dev, n, hd = self.device, k.shape[0], qk.head_dim
+        x = _dtype(k, _FLOATS)
+        y = x if q_out is None else _dtype(q_out, _FLOATS)
+        qs, ks = (n, qk.n_heads, hd), (n, qk.n_kv_heads, hd)
+        rc = self.lib.mrp_cache_append(self._h, self._raw_stream(), n, rows.ref, qk.typed(x, y), *_rows(q, "q", qs, x, dev),
+                                       *_rows(k, "k", ks, x, dev), *_rows(v, "v", ks, x, dev), cache.ref,
+                                       _dense(q_out, "q_out", y, qs, dev))
         return self._check(rc, "mrp_cache_append") if check else rc
 
-    def _attn(self, cfg: AttnCfg, q) -> _Attn:
-        return _Attn(cfg.n_heads, _dtype(q, "12"), cfg.scale, 1 if cfg.causal else 0, cfg.window, cfg.n_sink)
-
     def paged_attention_scratch_bytes(self, rows: NewRows, cache: PagedCache, cfg: AttnCfg, q) -> int:
-        return self.lib.mrp_paged_attention_scratch_bytes(self._h, q.shape[0], C.byref(rows.c), C.byref(cache.c),
-                                                          C.byref(self._attn(cfg, q)))
+        a = _Attn(cfg.n_heads, _dtype(q, _HALVES), cfg.scale, 1 if cfg.causal else 0, cfg.window, cfg.n_sink)
+        return self.lib.mrp_paged_attention_scratch_bytes(self._h, q.shape[0], rows.ref, cache.ref, C.byref(a))
 
     def paged_attention(self, rows: NewRows, cache: PagedCache, cfg: AttnCfg, q, out, lse=None, scratch=None,
                         check: bool = True) -> int:
         """out [n][n_heads][head_dim] (lse fp32 [n][n_heads], or None) of q over the cache.  scratch: a uint8 tensor of
         paged_attention_scratch_bytes, or None to take one from torch's allocator."""
-        import torch
-        n = q.shape[0]
-        self._here(q, out, lse, scratch, *rows.tensors, *cache.tensors)
+        self._here(rows, cache)
         if rows.B != cache.B:
             raise MrpError(f"{rows.B} sequences, but a page table of {cache.B}")
-        a = self._attn(cfg, q)
-        qp, qs = _row_tensor(q, "q", cfg.n_heads, cache.head_dim, n, a.dtype)
+        dev, n = self.device, q.shape[0]
+        y = _dtype(q, _HALVES)
+        shape = (n, cfg.n_heads, cache.head_dim)
         if scratch is None:
-            need = self.lib.mrp_paged_attention_scratch_bytes(self._h, n, C.byref(rows.c), C.byref(cache.c), C.byref(a))
-            scratch = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        rc = self.lib.mrp_paged_attention(self._h, _stream(), n, C.byref(rows.c), C.byref(cache.c), C.byref(a), qp, qs,
-                                          _plain(out, "out", str(a.dtype), (n, cfg.n_heads, cache.head_dim)),
-                                          _plain(lse, "lse", "0", (n, cfg.n_heads)), _ptr(scratch),
-                                          0 if scratch is None else scratch.numel() * scratch.element_size())
+            key = (n, cfg.n_heads, rows.shape, cache.shape)      # (all that the size depends on)
+            need = self._scratch_bytes.get(key)
+            if need is None:
+                if len(self._scratch_bytes) >= 4096:
+                    self._scratch_bytes.clear()
+                need = self._scratch_bytes[key] = self.paged_attention_scratch_bytes(rows, cache, cfg, q)
+            if need:
+                import torch
+                scratch = torch.empty(need, dtype=torch.uint8, device=q.device)
+        a = _Attn(cfg.n_heads, y, cfg.scale, 1 if cfg.causal else 0, cfg.window, cfg.n_sink)
+        rc = self.lib.mrp_paged_attention(self._h, self._raw_stream(), n, rows.ref, cache.ref, C.byref(a),
+                                          *_rows(q, "q", shape, y, dev), _dense(out, "out", y, shape, dev),
+                                          _dense(lse, "lse", 0, shape[:2], dev), *_scratch(scratch, dev))
         return self._check(rc, "mrp_paged_attention") if check else rc
 
     def profile_enable(self, on: bool):
