@@ -40,6 +40,33 @@ __device__ __forceinline__ void store8(void *base, long at, F16, const float (&x
     for (int e = 0; e < 8; ++e) v[e] = (_Float16)x[e];
     *reinterpret_cast<f16x8 *>(static_cast<uint16_t *>(base) + at) = v;
 }
+// Eight entries as they lie in memory, so that several requests are under way before the first is used
+template <typename T>
+struct Raw8 {
+    uint4 v[__is_same(T, F32) ? 2 : 1];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> raw8(const void *base, long at, T) {
+    Raw8<T> r;
+    const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(base) + at * (__is_same(T, F32) ? 4 : 2));
+    r.v[0] = p[0];
+    if constexpr (__is_same(T, F32)) r.v[1] = p[1];
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ void values8(const Raw8<T> &r, float (&x)[8]) {
+    if constexpr (__is_same(T, F32)) {
+        x[0] = __uint_as_float(r.v[0].x); x[1] = __uint_as_float(r.v[0].y); x[2] = __uint_as_float(r.v[0].z); x[3] = __uint_as_float(r.v[0].w);
+        x[4] = __uint_as_float(r.v[1].x); x[5] = __uint_as_float(r.v[1].y); x[6] = __uint_as_float(r.v[1].z); x[7] = __uint_as_float(r.v[1].w);
+    } else if constexpr (__is_same(T, BF16)) {
+        unpack_bf16x8(r.v[0], x);
+    } else {
+        const f16x8 h = __builtin_bit_cast(f16x8, r.v[0]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = (float)h[e];
+    }
+}
+
 // Round to nearest, ties to even; beyond 448 saturates, NaN stays
 __device__ __forceinline__ float e4m3_range(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
 __device__ __forceinline__ void store8_e4m3(void *base, long at, const float (&x)[8]) {

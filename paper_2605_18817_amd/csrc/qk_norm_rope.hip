@@ -154,44 +154,64 @@ __global__ __launch_bounds__(256) void qk_norm_rope_grad_kernel(const QkGrad A) 
         load_gain(gain, qk.gain_dtype, o0, g0);
         load_gain(gain, qk.gain_dtype, o1, g1);
     }
-    const long items = A.f.n_rows * heads;
-    for (long item = (long)w * per + threadIdx.x / tph; item < items; item += (long)nw * per) {
-        const long row = item / heads;
-        const int h = (int)(item - row * heads);
-        float a[8], b[8], t0[8], t1[8];
-        load8(dy, item * qk.head_dim + o0, YT{}, t0);
-        load8(dy, item * qk.head_dim + o1, YT{}, t1);
-        if (c < qk.rotary_dim / 16) {   // dn = R^T dy
-            const Turn t = load_turn(qk, clamp_pos(A.f.pos[row], qk.n_pos, A.f.err_flag), c);
+    const long items = A.f.n_rows * heads, step = (long)nw * per;
+    // two heads at a time: all that they read is asked for before the first is worked on
+    for (long item = (long)w * per + threadIdx.x / tph; item < items; item += 2 * step) {
+        Raw8<YT> y0[2], y1[2];
+        Raw8<XT> x0[2], x1[2];
+        long at[2];
+        int pos[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float u = t0[e], v = t1[e];
-                t0[e] = u * t.c[e] + v * t.s[e];
-                t1[e] = v * t.c[e] - u * t.s[e];
+        for (int u = 0; u < 2; ++u) {
+            const long it = item + u * step < items ? item + u * step : item, row = it / heads;
+            at[u] = (it - row * heads) * qk.head_dim;
+            pos[u] = qk.rotary_dim ? A.f.pos[row] : 0;
+            y0[u] = raw8(dy, it * qk.head_dim + o0, YT{});
+            y1[u] = raw8(dy, it * qk.head_dim + o1, YT{});
+            if (gain) {
+                x0[u] = raw8(x, row * stride + at[u] + o0, XT{});
+                x1[u] = raw8(x, row * stride + at[u] + o1, XT{});
             }
+            at[u] += row * dstride;
         }
-        if (gain) {
-            load8(x, row * stride + (long)h * qk.head_dim + o0, XT{}, a);
-            load8(x, row * stride + (long)h * qk.head_dim + o1, XT{}, b);
-            const float inv = 1.0f / sqrtf(head_sum(sum_squares(a, b), tph) / (float)qk.head_dim + qk.eps);
-            float dot = 0.f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                s0[e] += t0[e] * a[e] * inv;
-                s1[e] += t1[e] * b[e] * inv;
-                t0[e] *= g0[e];
-                t1[e] *= g1[e];
-                dot += t0[e] * a[e] + t1[e] * b[e];
-            }
-            const float m = head_sum(dot, tph) / (float)qk.head_dim * inv * inv;
+        for (int u = 0; u < 2; ++u) {
+            if (item + u * step >= items) break;   // (all threads of a head)
+            float a[8], b[8], t0[8], t1[8];
+            values8(y0[u], t0);
+            values8(y1[u], t1);
+            if (c < qk.rotary_dim / 16) {          // dn = R^T dy
+                const Turn t = load_turn(qk, clamp_pos(pos[u], qk.n_pos, A.f.err_flag), c);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                t0[e] = inv * (t0[e] - a[e] * m);
-                t1[e] = inv * (t1[e] - b[e] * m);
+                for (int e = 0; e < 8; ++e) {
+                    const float p = t0[e], q = t1[e];
+                    t0[e] = p * t.c[e] + q * t.s[e];
+                    t1[e] = q * t.c[e] - p * t.s[e];
+                }
             }
+            if (gain) {
+                values8(x0[u], a);
+                values8(x1[u], b);
+                const float inv = 1.0f / sqrtf(head_sum(sum_squares(a, b), tph) / (float)qk.head_dim + qk.eps);
+                float dot = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    s0[e] += t0[e] * a[e] * inv;
+                    s1[e] += t1[e] * b[e] * inv;
+                    t0[e] *= g0[e];
+                    t1[e] *= g1[e];
+                    dot += t0[e] * a[e] + t1[e] * b[e];
+                }
+                const float m = head_sum(dot, tph) / (float)qk.head_dim * inv * inv;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    t0[e] = inv * (t0[e] - a[e] * m);
+                    t1[e] = inv * (t1[e] - b[e] * m);
+                }
+            }
+            store8(dx, at[u] + o0, XT{}, t0);
+            store8(dx, at[u] + o1, XT{}, t1);
         }
-        store8(dx, row * dstride + (long)h * qk.head_dim + o0, XT{}, t0);
-        store8(dx, row * dstride + (long)h * qk.head_dim + o1, XT{}, t1);
     }
     if (!gain || !(is_q ? A.dq_gain : A.dk_gain)) return;
 #pragma unroll
@@ -211,21 +231,22 @@ __global__ __launch_bounds__(256) void qk_norm_rope_grad_kernel(const QkGrad A) 
     }
 }
 
-// The workgroups' sums in order: 16 threads take every 16th, then a tree over them
-__global__ __launch_bounds__(256) void gain_sum_kernel(const QkGrad A) {
-    __shared__ float sums[16][17];
+// The workgroups' sums: 64 threads on an entry take every 64th, then a tree over them (the order is the same in every call)
+__global__ __launch_bounds__(1024) void gain_sum_kernel(const QkGrad A) {
+    __shared__ float sums[64][17];
     const int hd = A.f.qk.head_dim, groups = hd / 16;
     const bool is_q = (int)blockIdx.x < groups;
     const int col = (is_q ? blockIdx.x : blockIdx.x - groups) * 16 + (threadIdx.x & 15), u = threadIdx.x >> 4;
     float *out = is_q ? A.dq_gain : A.dk_gain;
     if (!out || !(is_q ? A.f.qk.q_gain : A.f.qk.k_gain)) return;
-    const float *part = A.part + (is_q ? 0 : (size_t)A.wg_q * hd);
+    const float *part = A.part + (is_q ? 0 : (size_t)A.wg_q * hd) + col;
     const int n = is_q ? A.wg_q : A.wg_k;
     float s = 0.f;
-    for (int w = u; w < n; w += 16) s += part[(size_t)w * hd + col];
+#pragma unroll 4
+    for (int w = u; w < n; w += 64) s += part[(size_t)w * hd];
     sums[u][threadIdx.x & 15] = s;
     __syncthreads();
-    for (int half = 8; half > 0; half >>= 1) {
+    for (int half = 32; half > 0; half >>= 1) {
         if (u < half) sums[u][threadIdx.x & 15] += sums[u + half][threadIdx.x & 15];
         __syncthreads();
     }
@@ -255,6 +276,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const Append A) {
     const long row = item / heads;
     const int h = (int)(item - row * heads);
     if (row >= A.n_rows) return;
+    // what the thread takes of its head is on its way while the row is looked up
+    int o0, o1;
+    chunk_places(c, qk.rotary_dim, o0, o1);
+    const bool is_q = h < nq, is_k = h < nq + nkv;
+    const int hh = is_q ? h : (is_k ? h - nq : h - nq - nkv);
+    const void *src = is_q ? A.q : (is_k ? A.k : A.v);
+    const long from = row * (is_q ? A.q_stride : (is_k ? A.k_stride : A.v_stride)) + (long)hh * qk.head_dim;
+    const Raw8<XT> r0 = raw8(src, from + o0, XT{}), r1 = raw8(src, from + o1, XT{});
     // the row's sequence: the last one that begins at or before it
     int b;
     if (A.rows.cu_rows) {
@@ -273,17 +302,15 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const Append A) {
     const int i = (int)row - s.begin;
     if (i < 0 || i >= s.n) return;
     const int pos = s.len - s.n + i;
-    int o0, o1;
-    chunk_places(c, qk.rotary_dim, o0, o1);
     float x0[8], x1[8];
-    if (h < nq) {
-        const long at = row * A.q_stride + (long)h * qk.head_dim, to = (row * nq + h) * qk.head_dim;
+    values8(r0, x0);
+    values8(r1, x1);
+    if (is_q) {
+        const long to = (row * nq + h) * qk.head_dim;
         if (pos < 0) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) x0[e] = x1[e] = 0.f;
         } else {
-            load8(A.q, at + o0, XT{}, x0);
-            load8(A.q, at + o1, XT{}, x1);
             norm_turn(qk, qk.q_gain, pos, c, o0, o1, tph, A.err_flag, x0, x1);
         }
         store8(A.q_out, to + o0, YT{}, x0);
@@ -291,17 +318,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(const Append A) {
         return;
     }
     if (pos < 0) return;
-    const bool is_k = h < nq + nkv;
-    const int hh = is_k ? h - nq : h - nq - nkv;
-    const long at = row * (is_k ? A.k_stride : A.v_stride) + (long)hh * qk.head_dim;
     const int page = C.page_table[(size_t)b * C.max_pages + pos / C.page_size];
     if (page < 0 || page >= C.n_pages) {
         if (c == 0) atomicOr(A.err_flag, ERR_PAGE);
         return;
     }
-    const void *src = is_k ? A.k : A.v;
-    load8(src, at + o0, XT{}, x0);
-    load8(src, at + o1, XT{}, x1);
     if (is_k) norm_turn(qk, qk.k_gain, pos, c, o0, o1, tph, A.err_flag, x0, x1);
     const long slot = (long)page * C.page_size + pos % C.page_size;
     const long to = (slot * nkv + hh) * qk.head_dim;
@@ -403,10 +424,12 @@ int launched(mrp_ctx *c, const char *what) {
     return e == hipSuccess ? MRP_OK : ctx_fail(c, MRP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// Workgroups of the gradient on `items` heads: at most four per compute unit's worth, each with a sum of its own
-int grad_workgroups(long items, int head_dim) {
-    const long per = 256 / (head_dim / 16), n = (items + per - 1) / per;
-    return (int)(n > 1024 ? 1024 : n);
+// Workgroups of the gradient on the heads of q or of k, each with sums of its own: 1024 in all, shared out by the heads (four
+// on a compute unit; more are only more sums to add up)
+int grad_workgroups(long n_rows, int heads, int all_heads, int head_dim) {
+    const long per = 256 / (head_dim / 16), n = (n_rows * heads + per - 1) / per;
+    const long most = (1024L * heads + all_heads - 1) / all_heads;
+    return (int)(n > most ? most : n);
 }
 
 }  // namespace
@@ -482,7 +505,8 @@ int mrp_qk_norm_rope(mrp_ctx *c, void *stream, long n_rows, const mrp_qk *qk, co
 
 size_t mrp_qk_norm_rope_grad_scratch_bytes(long n_rows, const mrp_qk *qk) {
     if (!qk || n_rows <= 0 || n_rows > MAX_ROWS || qk->head_dim < 16 || qk->head_dim > 256 || qk->n_heads < 1 || qk->n_kv_heads < 0) return 0;
-    return (size_t)(grad_workgroups(n_rows * qk->n_heads, qk->head_dim) + grad_workgroups(n_rows * qk->n_kv_heads, qk->head_dim)) *
+    const int all = qk->n_heads + qk->n_kv_heads;
+    return (size_t)(grad_workgroups(n_rows, qk->n_heads, all, qk->head_dim) + grad_workgroups(n_rows, qk->n_kv_heads, all, qk->head_dim)) *
            qk->head_dim * sizeof(float);
 }
 
@@ -518,8 +542,9 @@ int mrp_qk_norm_rope_grad(mrp_ctx *c, void *stream, long n_rows, const mrp_qk *q
     QkGrad a;
     a.f = {*qk, n_rows, pos, q, k, q_stride, k_stride, const_cast<void *>(dq_out), const_cast<void *>(dk_out), ctx_view(c).err_flag};
     a.dq = dq; a.dk = dk; a.dq_stride = dq_stride; a.dk_stride = dk_stride;
-    a.wg_q = grad_workgroups(n_rows * qk->n_heads, qk->head_dim);
-    a.wg_k = grad_workgroups(n_rows * qk->n_kv_heads, qk->head_dim);
+    const int all = qk->n_heads + qk->n_kv_heads;
+    a.wg_q = grad_workgroups(n_rows, qk->n_heads, all, qk->head_dim);
+    a.wg_k = grad_workgroups(n_rows, qk->n_kv_heads, all, qk->head_dim);
     a.part = static_cast<float *>(scratch);
     a.dq_gain = dq_gain; a.dk_gain = dk_gain;
     if (n_rows > 0) {
@@ -528,7 +553,7 @@ int mrp_qk_norm_rope_grad(mrp_ctx *c, void *stream, long n_rows, const mrp_qk *q
         });
         CHECK(launched(c, what));
     }
-    if (dq_gain || dk_gain) gain_sum_kernel<<<2 * (qk->head_dim / 16), 256, 0, st>>>(a);
+    if (dq_gain || dk_gain) gain_sum_kernel<<<2 * (qk->head_dim / 16), 1024, 0, st>>>(a);
     return launched(c, what);
 }
 
