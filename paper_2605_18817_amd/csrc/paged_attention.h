@@ -7,7 +7,6 @@ namespace mrp {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // 2^x to one unit in the last place; below 2^-126: 0
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }

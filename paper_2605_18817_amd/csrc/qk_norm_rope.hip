@@ -116,8 +116,8 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkForward A) {
     const void *src = is_q ? A.q : A.k;
     const long at = row * (is_q ? A.q_stride : A.k_stride) + (long)hh * qk.head_dim;
     float a[8], b[8];
-    load8(src, at + o0, XT{}, a);
-    load8(src, at + o1, XT{}, b);
+    values8(raw8(src, at + o0, XT{}), a);
+    values8(raw8(src, at + o1, XT{}), b);
     norm_turn(qk, is_q ? qk.q_gain : qk.k_gain, qk.rotary_dim ? A.pos[row] : 0, c, o0, o1, tph, A.err_flag, a, b);
     void *dst = is_q ? A.q_out : A.k_out;
     const long to = (row * (is_q ? qk.n_heads : qk.n_kv_heads) + hh) * qk.head_dim;
