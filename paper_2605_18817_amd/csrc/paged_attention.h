@@ -93,8 +93,8 @@ __device__ __forceinline__ Words<N> load_words(const char *p) {
     if constexpr (N >= 4) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const uint4 v = reinterpret_cast<const uint4 *>(p)[i];
-            r.w[4 * i] = v.x; r.w[4 * i + 1] = v.y; r.w[4 * i + 2] = v.z; r.w[4 * i + 3] = v.w;
+            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i);
+            r.w[4 * i] = v[0]; r.w[4 * i + 1] = v[1]; r.w[4 * i + 2] = v[2]; r.w[4 * i + 3] = v[3];
         }
     } else if constexpr (N == 2) {
         const uint2 v = *reinterpret_cast<const uint2 *>(p);

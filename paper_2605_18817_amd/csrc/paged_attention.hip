@@ -207,7 +207,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                 return j < high ? table[j / C.page_size] : 0;
             };
             struct Raw {
-                uint4 k[2][NL];
+                u32x4 k[2][NL];
                 Words<NE * ES / 4> v[8];
                 uint32_t there;                // positions whose page is there
             };
@@ -225,7 +225,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int c = 0; c < NL; ++c) f.k[t][c] = *reinterpret_cast<const uint4 *>(kp + 4 * t * pitch + 64 * c);
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + 4 * t * pitch + 64 * c));
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vp + j * pitch);
                 } else {
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     for (int t = 0; t < 2; ++t) {
                         const char *kp = kb + __shfl(slot, 8 * (r16 >> 2) + 4 * t + (r16 & 3)) * pitch + 16 * g;
 #pragma unroll
-                        for (int c = 0; c < NL; ++c) f.k[t][c] = *reinterpret_cast<const uint4 *>(kp + 64 * c);
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + 64 * c));
                     }
 #pragma unroll
                     for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vb + __shfl(slot, 8 * g + j) * pitch + NE * ES * r16);
@@ -256,16 +256,16 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 #pragma unroll
                         for (int c = 0; c < NL; ++c) {
                             uint32_t a0, a1, a2, a3;
-                            widen(T{}, f.k[t][c].x, a0, a1);
-                            widen(T{}, f.k[t][c].y, a2, a3);
+                            widen(T{}, f.k[t][c][0], a0, a1);
+                            widen(T{}, f.k[t][c][1], a2, a3);
                             kf[2 * c] = u32x4{a0, a1, a2, a3};
-                            widen(T{}, f.k[t][c].z, a0, a1);
-                            widen(T{}, f.k[t][c].w, a2, a3);
+                            widen(T{}, f.k[t][c][2], a0, a1);
+                            widen(T{}, f.k[t][c][3], a2, a3);
                             kf[2 * c + 1] = u32x4{a0, a1, a2, a3};
                         }
                     } else {
 #pragma unroll
-                        for (int c = 0; c < NC; ++c) kf[c] = u32x4{f.k[t][c].x, f.k[t][c].y, f.k[t][c].z, f.k[t][c].w};
+                        for (int c = 0; c < NC; ++c) kf[c] = f.k[t][c];
                     }
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) {
