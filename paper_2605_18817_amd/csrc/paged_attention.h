@@ -82,6 +82,16 @@ __device__ __forceinline__ uint32_t seen_bits(int p, int key0, int len, const mr
     return seen;
 }
 
+// The larger of a lane's value and that of the lane 32 (16) from it
+__device__ __forceinline__ float max_halves(float x) {
+    const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+__device__ __forceinline__ float max_quarters(float x) {
+    const auto p = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(p[0]), __uint_as_float(p[1]));
+}
+
 // N dwords of a lane's share
 template <int N>
 struct Words {

@@ -305,8 +305,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     float mx = m[rt];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[rt][0][i], sc[rt][1][i]));
-                    mx = fmaxf(mx, __shfl_xor(mx, 16));
-                    mx = fmaxf(mx, __shfl_xor(mx, 32));
+                    mx = max_halves(max_quarters(mx));
                     const float ref = mx == -INFINITY ? 0.f : mx * c2;
                     if (__any(mx > m[rt])) {
                         const float alpha = exp2_(m[rt] * c2 - ref);

@@ -176,6 +176,12 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             }
         }
     };
+    int key_info[KN];                             // of a thread's pieces: where the place of their key is, and which part they are
+#pragma unroll
+    for (int n = 0; n < KN; ++n) {
+        const int x = (n * NW + wave) * 64 + lane, y = x / KS;
+        key_info[n] = 8 * ((y & 32) + row_key(y & 31)) | 16 * ((x % KS) ^ (y & (KS - 1))) << 16;
+    }
     uint4 kreg[KN];                               // (8 bits: keys are widened on their way; else they go to shared memory directly)
     uint32_t vreg[VK];
     // (a thread's values: entries DW vd .., vd = tid % VL, of keys VK vg .., vg = tid / VL)
@@ -192,9 +198,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         } else {
 #pragma unroll
             for (int n = 0; n < KN; ++n) {        // 64 pieces of a wave lie side by side
-                const int first = (n * NW + wave) * 64, y = (first + lane) / KS, part = ((first + lane) % KS) ^ (y & (KS - 1));
-                const long place = places[at][(y & 32) + row_key(y & 31)];
-                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + 16 * part + place), (las_ptr)(ks + 16 * first), 16, 0, 0);
+                const int first = (n * NW + wave) * 64;
+                const long place = *reinterpret_cast<const long *>(reinterpret_cast<const char *>(places[at]) + (key_info[n] & 0xffff));
+                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + (key_info[n] >> 16) + place), (las_ptr)(ks + 16 * first), 16, 0, 0);
             }
         }
         const char *const vp = vb + DW * ES * vd;
@@ -269,7 +275,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
-    auto compute = [&](int i, auto odd_tile) {
+    auto compute = [&](int i, auto odd_tile, auto after_scores, auto between) {
         const int lane = anew(threadIdx.x) & 63, r32 = lane & 31, h = lane >> 5, u = pc.begin + i, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         const int key0 = key_of(u);
@@ -287,6 +293,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             }
         }
         four_ahead<NT * NC>();
+        after_scores();
         const bool partial = is_partial(key0, th0, th1);
         if (partial) {
 #pragma unroll
@@ -300,7 +307,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         float mx = sc[0][0];
 #pragma unroll
         for (int i = 1; i < 16 * NT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        mx = max_halves(mx);
         // the sums are brought to a new reference where a score is more than a factor of 2^8 above the old one
         if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx > m))) {
             const float top = fmaxf(m, mx);
@@ -321,6 +328,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             p[i >> 3][(i & 7) >> 1] = pack2(T{}, p0, p1, x, y);
         }
         l += sum;
+        between();
         if (partial && odd[at]) {
             // A weight of zero times a value that is not finite is not zero.  Such values leave the product; how many of them a row
             // sees in an entry is a product too, of ones, and makes the row's entry NaN
@@ -384,13 +392,17 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     __syncthreads();
     auto step = [&](int i, auto odd_tile) {
         constexpr bool next = !decltype(odd_tile)::value;
-        if (i + 1 < n) request(i + 1, Odd<next>{});
-        if (i + 2 < n) {
-            look_up(i + 2);
-            if (i + 3 < n) ask(i + 3);
-        }
-        compute(i, odd_tile);
-        if (i + 1 < n) put(i + 1, Odd<next>{});
+        // The next tile is asked for while the scores' products are under way, and its values are put in place ahead of the second
+        // product: what a wave waits for is covered by what its matrix core does meanwhile
+        compute(i, odd_tile, [&] {
+            if (i + 1 < n) request(i + 1, Odd<next>{});
+            if (i + 2 < n) {
+                look_up(i + 2);
+                if (i + 3 < n) ask(i + 3);
+            }
+        }, [&] {
+            if (i + 1 < n) put(i + 1, Odd<next>{});
+        });
         __builtin_amdgcn_s_waitcnt(0x0F70);
         __syncthreads();
     };
