@@ -583,8 +583,10 @@ int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_row
     CHECK(check_cache(c, what, cache));
     if (attn->n_heads < 1 || attn->n_heads > 1024 || attn->n_heads % cache->n_kv_heads)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %d heads over %d key heads", what, attn->n_heads, cache->n_kv_heads);
-    if (n_rows * attn->n_heads > (1L << 28))
-        return ctx_fail(c, MRP_ERR_SHAPE, "%s: %ld rows of %d heads are too many", what, n_rows, attn->n_heads);
+    if (n_rows * attn->n_heads > (1L << 28) || most_rows(n_rows, *rows, attn->n_heads / cache->n_kv_heads) > (1L << 22) ||
+        (long)rows->B * cache->n_kv_heads > (1L << 22))
+        return ctx_fail(c, MRP_ERR_SHAPE, "%s: %ld rows of %d heads, %d sequences of %d key heads are too many", what, n_rows, attn->n_heads,
+                        rows->B, cache->n_kv_heads);
     if ((attn->dtype != MRP_DTYPE_BF16 && attn->dtype != MRP_DTYPE_F16) || (cache->dtype != MRP_DTYPE_E4M3 && cache->dtype != attn->dtype))
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: no form for type %d over a cache of type %d", what, attn->dtype, cache->dtype);
     if (!(attn->scale > 0.f) || attn->scale > 3e38f || attn->causal < 0 || attn->causal > 1 || attn->window < 0 || attn->n_sink < 0)

@@ -116,7 +116,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     const mrp_paged_cache &C = A.cache;
     const long cap = (long)C.max_pages * C.page_size;
     if (blockIdx.x == 0 && blockIdx.y == 0) check_rows(A.rows, A.n_rows, cap, A.err_flag, THREADS);
-    // key heads side by side: with eight of them, an XCD's L2 serves one.  The last rows, which have the most to do, come first.
+    // Key heads side by side: with eight of them, an XCD's L2 serves one, and one sequence at a time (two of 8083 and 5755 positions
+    // side by side: 837 us instead of 723).  The last rows, which have the most to do, come first.
     const int kvh = blockIdx.x % C.n_kv_heads, rest = blockIdx.x / C.n_kv_heads, b = blockIdx.y, G = A.G;
     const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
     const int nr = s.n * G, tiles = (nr + ROWS - 1) / ROWS;
