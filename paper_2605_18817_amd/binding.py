@@ -364,6 +364,10 @@ class AttnCfg:
     window: int = 0
     n_sink: int = 0
 
+    def __post_init__(self):
+        if not (0 <= self.window < 2 ** 31 and 0 <= self.n_sink < 2 ** 31):
+            raise MrpError(f"window={self.window} n_sink={self.n_sink} out of range")
+
 
 class StepIO:
     """Device buffers of one chain step (allocated with torch)."""

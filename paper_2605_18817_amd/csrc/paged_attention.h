@@ -97,13 +97,20 @@ template <int N>
 struct Words {
     uint32_t w[N];
 };
-template <int N>
+// (ONCE: nobody else asks for them)
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_16(const char *p) {
+    const u32x4 *q = reinterpret_cast<const u32x4 *>(p);
+    if constexpr (ONCE) return __builtin_nontemporal_load(q);
+    else return *q;
+}
+template <int N, bool ONCE>
 __device__ __forceinline__ Words<N> load_words(const char *p) {
     Words<N> r;
     if constexpr (N >= 4) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const u32x4 v = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p) + i);
+            const u32x4 v = load_16<ONCE>(p + 16 * i);
             r.w[4 * i] = v[0]; r.w[4 * i + 1] = v[1]; r.w[4 * i + 2] = v[2]; r.w[4 * i + 3] = v[3];
         }
     } else if constexpr (N == 2) {

@@ -74,13 +74,20 @@ __device__ __forceinline__ Ranges ranges_of(const Split &P, long total) {
 // partial results: per workgroup and place `rows` x (HD sums), then `rows` x (m, l)
 __host__ __device__ constexpr size_t place_floats(int rows, int HD) { return (size_t)rows * (HD + 2); }
 
-template <typename T, bool E8, int HD, int RT, bool AHEAD>
-__global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void paged_attention_kernel(const Attend A, const Split P, float *scratch, Pieces *items) {
+// RG: the waves of a workgroup are RG groups with 16 rows each, and those of a group take the steps in turn (waves of two groups
+// ask for the same keys and values, which come from memory once)
+template <typename T, bool E8, int HD, int RG>
+__global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention_kernel(const Attend A, const Split P, float *scratch, Pieces *items) {
     constexpr int ES = E8 ? 1 : 2;             // bytes of a cache entry
     constexpr int NC = HD / 32;                // contraction steps of a score
     constexpr int NE = HD / 16;                // entries of a lane's share of V, and A operands of O^T
     constexpr int NL = E8 ? NC / 2 : NC;       // 16-byte pieces of a lane's share of K
-    __shared__ float sm[WAVES][16 * RT], sl[WAVES][16 * RT];
+    constexpr int WK = WAVES / RG;             // waves of a group
+    constexpr int TILE = 16 * RG;              // rows of a workgroup
+    // A step's keys and values are asked for a turn ahead where they fit the registers twice (64 caches of up to 32767 positions of 8
+    // bits: 257 us without, 238 with it; 16 bits, 12 heads of 64: 325 without, 345 with it: two waves of a SIMD cover for each other)
+    constexpr bool AHEAD = E8 && HD <= 128;
+    __shared__ float sm[WAVES][16], sl[WAVES][16];
     __shared__ __align__(16) float so[WAVES][16][HD + 4];
     __shared__ long scan[WAVES];
     __shared__ long seq_base;
@@ -138,6 +145,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
     SeqRows s = seq_of;
 
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r16 = lane & 15, g = lane >> 4, G = A.G;
+    const int group = wave % RG, turn = wave / RG;
     const long pitch = (long)C.n_kv_heads * HD * ES;      // bytes between positions
     const bool whole = C.page_size % STEP == 0;           // a step lies in one page
     const bool causal = A.attn.causal != 0;
@@ -161,44 +169,38 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
             __syncthreads();                               // (the item before has been read out of shared memory)
 
             // the rows' positions and operands; lanes past the last row take it again and store nothing
-            int pos[RT];
-            u32x4 qf[RT][NC];
-            const int t_first = row0 / G, t_last = (row0 + 16 * RT < nr ? row0 + 16 * RT - 1 : nr - 1) / G;
+            int pos;
+            u32x4 qf[NC];
+            const int mine0 = row0 + 16 * group;      // the wave's first row
+            const int r = mine0 + r16 < nr ? mine0 + r16 : nr - 1;
+            const int t = r / G;
+            pos = s.len - s.n + t;
+            const uint16_t *qp = A.q + (long)(s.begin + t) * A.q_stride + (long)(kvh * G + r - t * G) * HD;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                const int r = row0 + 16 * rt + r16 < nr ? row0 + 16 * rt + r16 : nr - 1;
-                const int t = r / G;
-                pos[rt] = s.len - s.n + t;
-                const uint16_t *qp = A.q + (long)(s.begin + t) * A.q_stride + (long)(kvh * G + r - t * G) * HD;
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    // (8 bits: a lane's 16 bytes are 16 entries, for two contraction steps)
-                    const int at = E8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
-                    qf[rt][c] = *reinterpret_cast<const u32x4 *>(qp + at);
-                }
+            for (int c = 0; c < NC; ++c) {
+                // (8 bits: a lane's 16 bytes are 16 entries, for two contraction steps)
+                const int at = E8 ? 64 * (c >> 1) + 16 * g + 8 * (c & 1) : 32 * c + 8 * g;
+                qf[c] = *reinterpret_cast<const u32x4 *>(qp + at);
             }
 
-            // positions that any row sees: [0, sink) and [low, high); [full_low, full_high) is what all rows see
-            const int p_first = s.len - s.n + t_first, p_last = s.len - s.n + t_last;
-            const Steps st = steps_of<STEP>(A.attn, p_first, p_last, s.len);
-            const int low = st.low, high = st.high;
+            // positions that any row of the workgroup sees: [0, sink) and [low, high); [full_low, full_high) is what all of the wave's see
+            auto pos_of = [&](int r) { return s.len - s.n + (r < nr ? r : nr - 1) / G; };
+            const Steps st = steps_of<STEP>(A.attn, pos_of(row0), pos_of(row0 + TILE - 1), s.len);
+            const int low = st.low, high = st.high, p_first = pos_of(mine0), p_last = pos_of(mine0 + 15);
             const int full_high = p_first < 0 ? 0 : (causal ? p_first + 1 : s.len);
             const int full_low = W && p_last + 1 > W ? p_last + 1 - W : 0;
-            const int step_end = st.steps < unit1 * WAVES ? st.steps : unit1 * WAVES;
+            const int step_end = mine0 >= nr ? 0 : (st.steps < unit1 * WAVES ? st.steps : unit1 * WAVES);
 
             const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
             const char *kb = static_cast<const char *>(C.k_pages) + (long)kvh * HD * ES;
             const char *vb = static_cast<const char *>(C.v_pages) + (long)kvh * HD * ES;
 
-            float m[RT], l[RT];
-            f32x4 acc[RT][NE];
+            float m, l;
+            f32x4 acc[NE];
+            m = -INFINITY;
+            l = 0.f;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                m[rt] = -INFINITY;
-                l[rt] = 0.f;
-#pragma unroll
-                for (int e = 0; e < NE; ++e) acc[rt][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
+            for (int e = 0; e < NE; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
             auto key_of = [&](int u) { return (u < st.s_steps ? u : st.first + u - st.s_steps) * STEP; };
             // the page of step u's positions (of position key + lane % 32, where pages end inside a step), or -1
@@ -225,9 +227,9 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int c = 0; c < NL; ++c) f.k[t][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + 4 * t * pitch + 64 * c));
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = load_16<RG == 1>(kp + 4 * t * pitch + 64 * c);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vp + j * pitch);
+                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4, RG == 1>(vp + j * pitch);
                 } else {
                     const int j0 = key0 + (lane & 31);
                     const int slot = ok && j0 < high ? page * C.page_size + j0 % C.page_size : 0;
@@ -236,10 +238,10 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                     for (int t = 0; t < 2; ++t) {
                         const char *kp = kb + __shfl(slot, 8 * (r16 >> 2) + 4 * t + (r16 & 3)) * pitch + 16 * g;
 #pragma unroll
-                        for (int c = 0; c < NL; ++c) f.k[t][c] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + 64 * c));
+                        for (int c = 0; c < NL; ++c) f.k[t][c] = load_16<RG == 1>(kp + 64 * c);
                     }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4>(vb + __shfl(slot, 8 * g + j) * pitch + NE * ES * r16);
+                    for (int j = 0; j < 8; ++j) f.v[j] = load_words<NE * ES / 4, RG == 1>(vb + __shfl(slot, 8 * g + j) * pitch + NE * ES * r16);
                 }
             };
 
@@ -248,7 +250,7 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                 const uint32_t there = f.there;
                 if (there == 0) return;
                 const bool partial = there != 0xffffffffu || key0 + STEP > full_high || (key0 < full_low && key0 + STEP > sink);
-                f32x4 sc[RT][2];
+                f32x4 sc[2];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
                     u32x4 kf[NC];
@@ -267,12 +269,9 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 #pragma unroll
                         for (int c = 0; c < NC; ++c) kf[c] = f.k[t][c];
                     }
+                    sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        sc[rt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int c = 0; c < NC; ++c) sc[rt][t] = mfma(T{}, kf[c], qf[rt][c], sc[rt][t]);
-                    }
+                    for (int c = 0; c < NC; ++c) sc[t] = mfma(T{}, kf[c], qf[c], sc[t]);
                 }
                 uint32_t vw[8][NE / 2];
 #pragma unroll
@@ -288,45 +287,39 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 
                 if (partial) {
                     // scores of positions that a row does not see are dropped
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        const uint32_t seen = (seen_bits(pos[rt], key0, s.len, A.attn) & there) >> (8 * g);
-#pragma unroll
-                        for (int t = 0; t < 2; ++t)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) sc[rt][t][i] = (seen >> (4 * t + i)) & 1u ? sc[rt][t][i] : -INFINITY;
-                    }
-                }
-
-                // softmax of the step, and the weights as operands: the leading 16-bit term and the next
-                u32x4 ph[RT], pl[RT];
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt) {
-                    float mx = m[rt];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[rt][0][i], sc[rt][1][i]));
-                    mx = max_halves(max_quarters(mx));
-                    const float ref = mx == -INFINITY ? 0.f : mx * c2;
-                    if (__any(mx > m[rt])) {
-                        const float alpha = exp2_(m[rt] * c2 - ref);
-                        l[rt] *= alpha;
-#pragma unroll
-                        for (int e = 0; e < NE; ++e) acc[rt][e] *= alpha;
-                    }
-                    m[rt] = mx;
-                    float sum = 0.f;
+                    const uint32_t seen = (seen_bits(pos, key0, s.len, A.attn) & there) >> (8 * g);
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
-                        for (int i = 0; i < 4; i += 2) {
-                            const float p0 = exp2_(fmaf(sc[rt][t][i], c2, -ref)), p1 = exp2_(fmaf(sc[rt][t][i + 1], c2, -ref));
-                            float r0, r1, x, y;
-                            sum += p0 + p1;
-                            ph[rt][2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
-                            pl[rt][2 * t + i / 2] = pack2(T{}, r0, r1, x, y);
-                        }
-                    l[rt] += sum;
+                        for (int i = 0; i < 4; ++i) sc[t][i] = (seen >> (4 * t + i)) & 1u ? sc[t][i] : -INFINITY;
                 }
+
+                // softmax of the step, and the weights as operands: the leading 16-bit term and the next
+                u32x4 ph, pl;
+                float mx = m;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
+                mx = max_halves(max_quarters(mx));
+                const float ref = mx == -INFINITY ? 0.f : mx * c2;
+                if (__any(mx > m)) {
+                    const float alpha = exp2_(m * c2 - ref);
+                    l *= alpha;
+#pragma unroll
+                    for (int e = 0; e < NE; ++e) acc[e] *= alpha;
+                }
+                m = mx;
+                float sum = 0.f;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; i += 2) {
+                        const float p0 = exp2_(fmaf(sc[t][i], c2, -ref)), p1 = exp2_(fmaf(sc[t][i + 1], c2, -ref));
+                        float r0, r1, x, y;
+                        sum += p0 + p1;
+                        ph[2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
+                        pl[2 * t + i / 2] = pack2(T{}, r0, r1, x, y);
+                    }
+                l += sum;
 
                 bool bad = false;
                 if (partial) {                     // values that no row sees are cleared
@@ -351,21 +344,18 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
                 if (bad) {
                     // A weight of zero times a value that is not finite is not zero.  Such values leave the product; how many of them a
                     // row sees in an entry is a product too, of ones, and makes the row's entry NaN
+                    const uint32_t seen = seen_bits(pos, key0, s.len, A.attn) >> (8 * g);
+                    u32x4 sees;
 #pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        const uint32_t seen = seen_bits(pos[rt], key0, s.len, A.attn) >> (8 * g);
-                        u32x4 sees;
+                    for (int j = 0; j < 4; ++j) sees[j] = ((seen >> (2 * j)) & 1u) * one_bits(T{}) + (((seen >> (2 * j + 1)) & 1u) * one_bits(T{}) << 16);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) sees[j] = ((seen >> (2 * j)) & 1u) * one_bits(T{}) + (((seen >> (2 * j + 1)) & 1u) * one_bits(T{}) << 16);
+                    for (int e = 0; e < NE; ++e) {
+                        u32x4 other = turned(e);
 #pragma unroll
-                        for (int e = 0; e < NE; ++e) {
-                            u32x4 other = turned(e);
+                        for (int k = 0; k < 4; ++k) other[k] = odd_halves(T{}, other[k]);
+                        const f32x4 count = mfma(T{}, other, sees, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) other[k] = odd_halves(T{}, other[k]);
-                            const f32x4 count = mfma(T{}, other, sees, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[rt][e][i] = count[i] > 0.f ? NAN : acc[rt][e][i];
-                        }
+                        for (int i = 0; i < 4; ++i) acc[e][i] = count[i] > 0.f ? NAN : acc[e][i];
                     }
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -375,89 +365,86 @@ __global__ __launch_bounds__(64 * WAVES, RT == 1 && HD <= 128 ? 2 : 1) void page
 #pragma unroll
                 for (int e = 0; e < NE; ++e) {
                     const u32x4 vt = turned(e);
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) {
-                        acc[rt][e] = mfma(T{}, vt, ph[rt], acc[rt][e]);
-                        if constexpr (RT <= 2) acc[rt][e] = mfma(T{}, vt, pl[rt], acc[rt][e]);
-                    }
+                    acc[e] = mfma(T{}, vt, ph, acc[e]);
+                    acc[e] = mfma(T{}, vt, pl, acc[e]);
                 }
             };
 
             {
-                int u = unit0 * WAVES + wave;
-                int page1 = u < step_end ? page_of(u) : 0, page2 = u + WAVES < step_end ? page_of(u + WAVES) : 0;
+                int u = unit0 * WAVES + turn;
+                int page1 = u < step_end ? page_of(u) : 0, page2 = u + WK < step_end ? page_of(u + WK) : 0;
                 if constexpr (AHEAD) {
                     Raw f;
                     if (u < step_end) request(u, page1, f);
-                    for (; u < step_end; u += WAVES) {
+                    for (; u < step_end; u += WK) {
                         Raw next;
-                        const bool more = u + WAVES < step_end;
-                        if (more) request(u + WAVES, page2, next);
-                        if (u + 2 * WAVES < step_end) page2 = page_of(u + 2 * WAVES);
+                        const bool more = u + WK < step_end;
+                        if (more) request(u + WK, page2, next);
+                        if (u + 2 * WK < step_end) page2 = page_of(u + 2 * WK);
                         compute(u, f);
                         if (more) f = next;
                     }
                 } else {
-                    for (; u < step_end; u += WAVES) {
+                    for (; u < step_end; u += WK) {
                         Raw f;
                         request(u, page1, f);
                         page1 = page2;
-                        if (u + 2 * WAVES < step_end) page2 = page_of(u + 2 * WAVES);
+                        if (u + 2 * WK < step_end) page2 = page_of(u + 2 * WK);
                         compute(u, f);
                     }
                 }
             }
 
             // the four lanes of a row add up their sums, the waves their rows
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                l[rt] += __shfl_xor(l[rt], 16);
-                l[rt] += __shfl_xor(l[rt], 32);
-                if (g == 0) {
-                    sm[wave][16 * rt + r16] = m[rt];
-                    sl[wave][16 * rt + r16] = l[rt];
-                }
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            if (g == 0) {
+                sm[wave][r16] = m;
+                sl[wave][r16] = l;
             }
             const bool all = unit0 == 0 && unit1 == units;
             float *const place = all ? nullptr : scratch + ((size_t)blockIdx.x * 2 + (unit0 == 0 ? 1 : 0)) * place_floats(P.rows, HD);
             const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
+            __syncthreads();
+            {
+                float mx = -INFINITY;
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) {
-                __syncthreads();
-                {
-                    float mx = -INFINITY;
+                for (int w = 0; w < WK; ++w) mx = fmaxf(mx, sm[group + RG * w][r16]);
+                const float f = m == -INFINITY ? 0.f : exp2_((m - mx) * c2);
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + r16]);
-                    const float f = m[rt] == -INFINITY ? 0.f : exp2_((m[rt] - mx) * c2);
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int e = 0; e < NE; e += 4)
+                        *reinterpret_cast<float4 *>(&so[wave][r16][NE * (4 * g + i) + e]) =
+                            make_float4(acc[e][i] * f, acc[e + 1][i] * f, acc[e + 2][i] * f, acc[e + 3][i] * f);
+            }
+            __syncthreads();
+            const int rr = threadIdx.x >> 4, part = threadIdx.x & 15;
 #pragma unroll
-                        for (int e = 0; e < NE; e += 4)
-                            *reinterpret_cast<float4 *>(&so[wave][r16][NE * (4 * g + i) + e]) =
-                                make_float4(acc[rt][e][i] * f, acc[rt][e + 1][i] * f, acc[rt][e + 2][i] * f, acc[rt][e + 3][i] * f);
+            for (int q = 0; q < RG; ++q) {
+                const int at = 16 * q + rr, r = row0 + at;
+                if (r >= nr) break;
+                float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WK; ++w) mx = fmaxf(mx, sm[q + RG * w][rr]);
+                float o[NE];
+#pragma unroll
+                for (int e = 0; e < NE; ++e) o[e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < WK; ++w) {
+                    const float mw = sm[q + RG * w][rr];
+                    if (mw != -INFINITY) sum += sl[q + RG * w][rr] * exp2_((mw - mx) * c2);
+#pragma unroll
+                    for (int e = 0; e < NE; ++e) o[e] += so[q + RG * w][rr][NE * part + e];
                 }
-                __syncthreads();
-                const int rr = threadIdx.x >> 4, part = threadIdx.x & 15, r = row0 + 16 * rt + rr;
-                if (r < nr) {
-                    float mx = -INFINITY, sum = 0.f;
+                if (all) {
+                    const int t = r / G;
+                    store_row<T, HD>(A, s.begin + t, kvh * G + r - t * G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
+                } else {
+                    float4 *dst = reinterpret_cast<float4 *>(place + (size_t)at * HD + NE * part);
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) mx = fmaxf(mx, sm[w][16 * rt + rr]);
-#pragma unroll
-                    for (int w = 0; w < WAVES; ++w)
-                        if (sm[w][16 * rt + rr] != -INFINITY) sum += sl[w][16 * rt + rr] * exp2_((sm[w][16 * rt + rr] - mx) * c2);
-                    float o[NE];
-#pragma unroll
-                    for (int e = 0; e < NE; ++e)
-                        o[e] = ((so[0][rr][NE * part + e] + so[1][rr][NE * part + e]) + so[2][rr][NE * part + e]) + so[3][rr][NE * part + e];
-                    if (all) {
-                        const int t = r / G;
-                        store_row<T, HD>(A, s.begin + t, kvh * G + r - t * G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
-                    } else {
-                        float4 *dst = reinterpret_cast<float4 *>(place + (size_t)(16 * rt + rr) * HD + NE * part);
-#pragma unroll
-                        for (int e = 0; e < NE; e += 4) dst[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
-                        if (part == 0) *reinterpret_cast<float2 *>(place + (size_t)P.rows * HD + 2 * (16 * rt + rr)) = make_float2(mx, sum);
-                    }
+                    for (int e = 0; e < NE; e += 4) dst[e / 4] = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                    if (part == 0) *reinterpret_cast<float2 *>(place + (size_t)P.rows * HD + 2 * at) = make_float2(mx, sum);
                 }
             }
         }
@@ -523,19 +510,20 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend 
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
-// Rows of a tile: the fewest that hold a sequence's rows, up to 32.  The largest number of workgroups is what fits the device at
-// once: two a compute unit for 16 rows of up to 128 entries, else one
+// Rows of a workgroup: the fewest of 16, 32, 64 that hold a sequence's (more than 32 of up to 128 entries are not this kernel's).  The
+// largest number of workgroups is what fits the device at once: two a compute unit, one for heads of 256.
 Split split_of(long rows, int HD, int nCU) {
-    const int tr = rows <= 16 ? 16 : 32;
-    return Split{tr, ceil_div(rows, tr), (tr == 16 && HD <= 128 ? 2 : 1) * (nCU > 0 ? nCU : 1)};
+    const int tr = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
+    return Split{tr, ceil_div(rows, tr), (HD <= 128 ? 2 : 1) * (nCU > 0 ? nCU : 1)};
 }
 size_t partial_floats(const Split &p, int HD) { return 2 * (size_t)p.workgroups * place_floats(p.rows, HD); }
 
 template <typename T, bool E8, int HD>
 void launch(const Attend &a, const Split &p, float *scratch, hipStream_t st) {
     Pieces *const items = reinterpret_cast<Pieces *>(scratch + partial_floats(p, HD));
-    if (p.rows == 16) paged_attention_kernel<T, E8, HD, 1, false><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
-    else paged_attention_kernel<T, E8, HD, 2, false><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
+    if (p.rows == 16) paged_attention_kernel<T, E8, HD, 1><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
+    else if (HD <= 128 || p.rows == 32) paged_attention_kernel<T, E8, HD, 2><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
+    else if constexpr (HD == 256) paged_attention_kernel<T, E8, HD, 4><<<p.workgroups, 64 * WAVES, 0, st>>>(a, p, scratch, items);
     paged_attention_join_kernel<T, E8, HD><<<dim3(p.tiles * a.cache.n_kv_heads, a.rows.B), 256, 0, st>>>(a, p, scratch, items);
 }
 
@@ -601,8 +589,9 @@ int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_row
     if (need && !scratch) return ctx_fail(c, MRP_ERR_NULL, "%s: scratch is NULL", what);
     if (scratch_bytes < need) return ctx_fail(c, MRP_ERR_WORKSPACE, "%s: scratch holds %zu of %zu bytes", what, scratch_bytes, need);
     CHECK(check_context_device(c, what));
-    const Attend a = {*rows, *cache, *attn, (int)n_rows, attn->n_heads / cache->n_kv_heads, static_cast<const uint16_t *>(q), q_stride,
+    Attend a = {*rows, *cache, *attn, (int)n_rows, attn->n_heads / cache->n_kv_heads, static_cast<const uint16_t *>(q), q_stride,
                       static_cast<uint16_t *>(out), lse, ctx_view(c).err_flag};
+    if (attn->window > (long)cache->max_pages * cache->page_size) a.attn.window = 0;   // (wider than any sequence: none)
     hipStream_t st = static_cast<hipStream_t>(stream);
     if (prompt_takes(most_rows(n_rows, *rows, a.G), cache->head_dim)) {
         const hipError_t e = launch_prompt_attention(a, static_cast<float *>(scratch), ctx_view(c).nCU, st);

@@ -536,6 +536,9 @@ void launch_hd(const Attend &a, const Cut &c, int rows, float *scratch, hipStrea
 
 }  // namespace
 
+// From 33 rows of a key head.  64 rows here / in paged_attention.hip's kernel (four waves, 16 rows each): 64 caches of up to 32767
+// positions, bf16, 672 / 704 us; 32 of up to 8000, e4m3, 96 / 135.  32 rows there: 469, bf16.  (Heads of 256 stay there: their sums and
+// queries would not fit a wave's registers here.)
 bool prompt_takes(long rows, int head_dim) { return rows > 32 && head_dim <= 128; }
 
 size_t prompt_scratch_floats(long rows, int B, int n_kv_heads, long positions, int head_dim, int nCU) {

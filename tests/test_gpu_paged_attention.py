@@ -65,10 +65,11 @@ def test_single_tokens(ctx, H, Hkv, hd, dtype, cache, window, sinks):
 
 @pytest.mark.parametrize("page", [1, 3, 16, 48, 64, 1000])
 @pytest.mark.parametrize("causal,window,sinks", [(True, 0, 0), (False, 0, 0), (True, 40, 3), (False, 33, 0), (True, 1, 70), (True, 64, 64)])
-def test_blocks_pages_and_windows(ctx, page, causal, window, sinks):
+@pytest.mark.parametrize("H,hd,dtype,cache", [(8, 128, "bf16", "bf16"), (16, 128, "f16", "e4m3"), (16, 64, "bf16", "bf16")])     # 32 and 64 rows of a key head
+def test_blocks_pages_and_windows(ctx, page, causal, window, sinks, H, hd, dtype, cache):
     lens = [4, 16, 17, 40, 100, 257, 1]
     new = [4, 16, 1, 7, 16, 16, 1]
-    _run(ctx, ref.Batch(new, lens, page, behind=2), 8, 4, 128, "bf16", "bf16", causal, window, sinks)
+    _run(ctx, ref.Batch(new, lens, page, behind=2), H, 4, hd, dtype, cache, causal, window, sinks)
 
 
 @pytest.mark.parametrize("H,Hkv,hd,dtype,cache", [(8, 2, 128, "bf16", "bf16"), (4, 1, 64, "f16", "f16"), (4, 4, 256, "bf16", "bf16"),
@@ -175,9 +176,17 @@ def test_long_caches(ctx, new, lens):
     _run(ctx, ref.Batch(new, lens, 64), 8, 2, 128, "bf16", "bf16", causal=len(new) > 1)
 
 
-def test_many_sequences(ctx):
+@pytest.mark.parametrize("window,sinks", [(0, 0), (3000, 70), (2 ** 31 - 1, 5)])
+def test_long_prompts_in_pieces(ctx, window, sinks):
+    """Few workgroups over a long cache: the positions are cut into pieces and joined; a window wider than any sequence is none."""
+    _run(ctx, ref.Batch([100, 9], [9100, 700], 32), 4, 1, 64, "f16", "f16", True, window, sinks)
+
+
+@pytest.mark.parametrize("uniform", [True, False])
+def test_many_sequences(ctx, uniform):
     lens = [1 + (37 * b) % 150 for b in range(700)]
-    _run(ctx, ref.Batch([1] * 700, lens, 16, uniform=True), 4, 2, 64, "bf16", "bf16")
+    new = [1] * 700 if uniform else [(b * 7) % 3 for b in range(700)]
+    _run(ctx, ref.Batch(new, lens, 16, uniform=uniform), 4, 2, 64, "bf16", "bf16")
 
 
 def test_strided_queries_and_shared_pages(ctx):
