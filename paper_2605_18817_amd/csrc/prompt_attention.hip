@@ -8,8 +8,12 @@
 //     O^T += V^T P^T  (A = 32 entries x 16 keys, B = 16 keys x 32 rows)
 // The result of the first product has keys 8 (i / 4) + 4 h + i % 4 of row r in registers i of lane 32 h + r, the second wants keys 8 h ..
 // 8 h + 7 of every 16: a tile's keys lie in shared memory in the order that makes these the same, and the weights stay in
-// their lanes.  Values are turned on their way into shared memory: entry d of all keys in row 'd / 2, odd entries behind the even
-// ones', so that a lane ends up with neighbouring entries of its output row.
+// their lanes.  Values are turned on their way into shared memory: entry d of all keys in row d / 2, the odd entries' rows behind the
+// even ones', so that a lane ends up with neighbouring entries of its output row.
+//
+// Two prompts of 4096 and 3565 rows behind 3987 and 2190 positions, 32 heads of 128 over 8: 637 GFLOP in 736 us, 870 TFLOP/s.  A tile costs a
+// wave 1024 cycles of the matrix core and about as many of the vector unit, 2740 in all for each of the two waves of a SIMD: within
+// a wave they follow each other.  256 rows a workgroup rather than 128: 749 against 826 us, whose tiles are fetched and turned twice as often.
 #include "paged_attention.h"
 
 namespace mrp {
