@@ -109,6 +109,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     constexpr int DW = E8 ? 4 : 2;                // entries of a value that a thread takes
     constexpr int VL = HD / DW;                   // threads on a value
     constexpr int VK = KT * VL / THREADS;         // keys of a thread
+    constexpr bool EARLY = KH == 2;
     static_assert(VK >= 2 && VK <= 16, "a thread's share");
     // (two variables, and the loop takes the tiles in pairs: what is on its way into one is then seen not to touch the other)
     __shared__ __align__(16) char ks_even[KT * KROW], ks_odd[KT * KROW];
@@ -191,21 +192,25 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     uint32_t vreg[VK];
     // (a thread's values: entries DW vd .., vd = tid % VL, of keys VK vg .., vg = tid / VL)
     // (what follows from a thread's number is worked out for each tile: kept, it would take the registers that the tile needs)
-    auto request = [&](int i, auto odd_tile) {
-        const int tid = anew(threadIdx.x), lane = tid & 63, vd = tid % VL, vg = tid / VL, at = i & 3;
-        char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even;
+    auto request_direct = [&](int i, auto odd_tile) {
+        if constexpr (!E8) {
+            char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even;
+#pragma unroll
+            for (int n = 0; n < KN; ++n) {        // 64 pieces of a wave lie side by side
+                const int first = (n * NW + wave) * 64;
+                const long place = *reinterpret_cast<const long *>(reinterpret_cast<const char *>(places[i & 3]) + (key_info[n] & 0xffff));
+                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + (key_info[n] >> 16) + place), (las_ptr)(ks + 16 * first), 16, 0, 0);
+            }
+            asm volatile("" ::: "memory");        // (what is asked for after it stays after it: the waits count)
+        }
+    };
+    auto request = [&](int i) {
+        const int tid = anew(threadIdx.x), vd = tid % VL, vg = tid / VL, at = i & 3;
         if constexpr (E8) {
 #pragma unroll
             for (int n = 0; n < KN && (K_ALL || tid < KT * KP); ++n) {
                 const int key = (tid + n * THREADS) / KP, part = (tid + n * THREADS) % KP;
                 kreg[n] = *reinterpret_cast<const uint4 *>(kb + 16 * part + places[at][key]);
-            }
-        } else {
-#pragma unroll
-            for (int n = 0; n < KN; ++n) {        // 64 pieces of a wave lie side by side
-                const int first = (n * NW + wave) * 64;
-                const long place = *reinterpret_cast<const long *>(reinterpret_cast<const char *>(places[at]) + (key_info[n] & 0xffff));
-                __builtin_amdgcn_global_load_lds((gas_ptr)(kb + (key_info[n] >> 16) + place), (las_ptr)(ks + 16 * first), 16, 0, 0);
             }
         }
         const char *const vp = vb + DW * ES * vd;
@@ -389,26 +394,44 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         ask(1);
         if (n > 1) look_up(1);
         ask(2);
+        if (EARLY) {
+            if (n > 2) look_up(2);
+            ask(3);
+        }
         __syncthreads();
-        request(0, Even{});
+        request_direct(0, Even{});
+        request(0);
         put(0, Even{});
+        if (EARLY && n > 1) request(1);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): what goes to shared memory directly is there
     __syncthreads();
     auto step = [&](int i, auto odd_tile) {
-        constexpr bool next = !decltype(odd_tile)::value;
+        using Next = Odd<!decltype(odd_tile)::value>;
         // The next tile is asked for while the scores' products are under way, and its values are put in place ahead of the second
-        // product: what a wave waits for is covered by what its matrix core does meanwhile
+        // product: what a wave waits for is covered by what its matrix core does meanwhile.  EARLY: values (and keys of 8 bits) are
+        // asked for a tile before that, since a tile's work is shorter than the memory takes; keys that go to shared memory
+        // directly at the tile's begin
+        if (EARLY && i + 1 < n) request_direct(i + 1, Next{});
         compute(i, odd_tile, [&] {
-            if (i + 1 < n) request(i + 1, Odd<next>{});
-            if (i + 2 < n) {
-                look_up(i + 2);
+            if (EARLY) {
+                if (i + 3 < n) look_up(i + 3);
+                if (i + 4 < n) ask(i + 4);
+            } else {
+                if (i + 1 < n) {
+                    request_direct(i + 1, Next{});
+                    request(i + 1);
+                }
+                if (i + 2 < n) look_up(i + 2);
                 if (i + 3 < n) ask(i + 3);
             }
         }, [&] {
-            if (i + 1 < n) put(i + 1, Odd<next>{});
+            if (i + 1 < n) put(i + 1, Next{});
+            if (EARLY && i + 2 < n) request(i + 2);
         });
-        __builtin_amdgcn_s_waitcnt(0x0F70);
+        // the keys that go to shared memory directly are there: nothing is on its way but the VK values asked for after them
+        if (!EARLY || i + 2 >= n) __builtin_amdgcn_s_waitcnt(0x0F70);
+        else if (!E8) __builtin_amdgcn_s_waitcnt(0x0F70 | (VK & 15) | (VK >> 4 << 14));
         __syncthreads();
     };
     for (int i = 0; i < n; i += 2) {
