@@ -37,7 +37,8 @@ using Even = Odd<false>;
 
 struct Cut {
     int tiles;       // row tiles that a sequence can have
-    int pieces;      // parts of the positions, joined by a second kernel where there is more than one
+    int pieces;      // parts of a row tile's positions, at most; joined by a second kernel where there are more than one
+    int slots;       // pieces that the whole batch is cut into, about
 };
 
 typedef const __attribute__((address_space(1))) void *gas_ptr;
@@ -54,18 +55,55 @@ __device__ __forceinline__ int row_key(int y) {
     return 16 * (i >> 3) + 8 * h + (i & 7);
 }
 
-// The tiles of a piece of a row tile
-struct Piece {
-    Steps st;
-    int begin, end;
-};
-__device__ __forceinline__ Piece piece_of(const Attend &A, const SeqRows &s, int row0, int rows, int nr, int pieces, int piece) {
-    Piece p;
-    const int last = row0 + rows < nr ? row0 + rows - 1 : nr - 1;
-    p.st = steps_of<KT>(A.attn, s.len - s.n + row0 / A.G, s.len - s.n + last / A.G, s.len);
-    p.begin = (int)((long)p.st.steps * piece / pieces);
-    p.end = (int)((long)p.st.steps * (piece + 1) / pieces);
-    return p;
+// Partial results: per row tile and piece ROWS x (HD sums), then ROWS x (reference, sum of weights); behind them the pieces' size
+__host__ __device__ inline size_t pieces_floats(int B, const Cut &P, int n_kv_heads, int rows, int HD) {
+    return (size_t)B * P.tiles * n_kv_heads * P.pieces * rows * (HD + 2);
+}
+__device__ __forceinline__ int *size_place(const Attend &A, const Cut &P, float *scratch, int rows, int HD) {
+    return reinterpret_cast<int *>(scratch + pieces_floats(A.rows.B, P, A.cache.n_kv_heads, rows, HD));
+}
+
+// Where the positions of 64 rows are cut: into as many parts for each sequence (32 caches of up to 8000 positions of 8 bits: 96 us; cut as
+// below 117 to 126, whose few longer parts come in rounds)
+__device__ __forceinline__ int even_size(int steps, int pieces) {
+    const int size = (steps + pieces - 1) / pieces;
+    return size < 1 ? 1 : size;
+}
+
+// Where the positions of more rows are cut: every so many tiles of them, the same for the whole batch, so that its pieces are about as
+// many as find a place on the device, and none has to take longer than the others.  Worked out by all threads of a workgroup.
+template <int THREADS>
+__device__ __forceinline__ int piece_size(const Attend &A, const Cut &P, int rows, long cap) {
+    __shared__ long totals[THREADS / 64];
+    __shared__ int longest[THREADS / 64];
+    long total = 0;
+    int most = 0;
+    for (int i = threadIdx.x; i < A.rows.B; i += THREADS) {
+        const SeqRows s = seq_rows(A.rows, A.n_rows, cap, i);
+        if (s.n == 0) continue;
+        const int steps = steps_of<KT>(A.attn, s.len - s.n, s.len - 1, s.len).steps;
+        total += (long)steps * ((s.n * A.G + rows - 1) / rows);
+        most = most > steps ? most : steps;
+    }
+    for (int off = 32; off > 0; off >>= 1) {
+        total += __shfl_xor(total, off);
+        const int other = __shfl_xor(most, off);
+        most = most > other ? most : other;
+    }
+    if ((threadIdx.x & 63) == 0) {
+        totals[threadIdx.x >> 6] = total;
+        longest[threadIdx.x >> 6] = most;
+    }
+    __syncthreads();
+    total = 0;
+    most = 0;
+    for (int w = 0; w < THREADS / 64; ++w) {
+        total += totals[w];
+        most = most > longest[w] ? most : longest[w];
+    }
+    const long even = (total * A.cache.n_kv_heads + P.slots - 1) / P.slots, least = (most + P.pieces - 1) / P.pieces;
+    const long size = even > least ? even : least;
+    return size < 4 ? 4 : (int)size;
 }
 
 // x, hidden from what moves constant work out of loops
@@ -127,10 +165,19 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     const SeqRows s = seq_rows(A.rows, A.n_rows, cap, b);
     const int nr = s.n * G, tiles = (nr + ROWS - 1) / ROWS;
     const int piece = rest % P.pieces, tile = tiles - 1 - rest / P.pieces;
+    int size = 0x7fffffff;
+    if (KH == 1 && P.pieces > 1) {
+        size = piece_size<THREADS>(A, P, ROWS, cap);
+        if (blockIdx.x == 0 && b == 0 && threadIdx.x == 0) *size_place(A, P, scratch, ROWS, HD) = size;   // (for the join)
+    }
     if (tile < 0) return;
-    const int row0 = tile * ROWS;
-    const Piece pc = piece_of(A, s, row0, ROWS, nr, P.pieces, piece);
-    const Steps &st = pc.st;
+    const int row0 = tile * ROWS, last = row0 + ROWS < nr ? row0 + ROWS - 1 : nr - 1;
+    const Steps st = steps_of<KT>(A.attn, s.len - s.n + row0 / G, s.len - s.n + last / G, s.len);
+    if (KH == 2) size = even_size(st.steps, P.pieces);
+    const bool pieces = st.steps > size;          // more than one
+    const int begin = piece ? (int)((long)piece * size < st.steps ? piece * size : st.steps) : 0;
+    const int n = (st.steps - begin < size ? st.steps - begin : size);
+    if (piece && n == 0) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, r32 = lane & 31, h = lane >> 5;
     const int part = wave % (NW / KH), half = wave / (NW / KH);   // of the rows, and of a tile's keys
 
@@ -160,17 +207,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         return (th0 & th1) != 0xffffffffu || key0 + KT > full_high || (key0 < full_low && key0 + KT > sink);
     };
     // The first wave looks up the places of the piece's tile i: it asks for the page numbers a turn before it needs them
-    int page = 0;
     auto ask = [&](int i) {
-        if (wave == 0) {
-            const int j = key_of(pc.begin + i) + lane;
-            page = j < st.high ? table[j / C.page_size] : -1;
-        }
+        const int j = key_of(begin + i) + lane;
+        return wave == 0 && j < st.high ? table[j / C.page_size] : -1;
     };
-    auto look_up = [&](int i) {
+    auto look_up = [&](int i, int page) {
         const int at = i & 3;
         if (wave == 0) {
-            const int j = key_of(pc.begin + i) + lane;
+            const int j = key_of(begin + i) + lane;
             const bool ok = page >= 0 && page < C.n_pages;
             if (!ok && j < st.high) atomicOr(A.err_flag, ERR_PAGE);
             places[at][lane] = ok ? ((long)page * C.page_size + j % C.page_size) * pitch : 0;
@@ -218,7 +262,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         for (int n = 0; n < VK; ++n) vreg[n] = load_part<DW * ES>(vp + places[at][VK * vg + n]);
     };
     auto put = [&](int i, auto odd_tile) {
-        const int tid = anew(threadIdx.x), vd = tid % VL, vg = tid / VL, u = pc.begin + i, at = i & 3;
+        const int tid = anew(threadIdx.x), vd = tid % VL, vg = tid / VL, u = begin + i, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         if constexpr (E8) {
 #pragma unroll
@@ -286,7 +330,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
 
     auto compute = [&](int i, auto odd_tile, auto after_scores, auto between) {
-        const int lane = anew(threadIdx.x) & 63, r32 = lane & 31, h = lane >> 5, u = pc.begin + i, at = i & 3;
+        const int lane = anew(threadIdx.x) & 63, r32 = lane & 31, h = lane >> 5, u = begin + i, at = i & 3;
         char *const ks = decltype(odd_tile)::value ? ks_odd : ks_even, *const vs = decltype(odd_tile)::value ? vs_odd : vs_even;
         const int key0 = key_of(u);
         const uint32_t th0 = there[at][0], th1 = there[at][1];
@@ -387,24 +431,22 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     };
 
     // three tiles are on their way: the places of the one after the next, keys and values of the next, and the one at work
-    const int n = pc.end - pc.begin;
+    int page = -1;                                // of the tile that is looked up next
     if (n > 0) {
-        ask(0);
-        look_up(0);
-        ask(1);
-        if (n > 1) look_up(1);
-        ask(2);
-        if (EARLY) {
-            if (n > 2) look_up(2);
-            ask(3);
-        }
+        const int page0 = ask(0), page1 = ask(1), page2 = ask(2), page3 = EARLY ? ask(3) : -1;
+        look_up(0, page0);
+        if (n > 1) look_up(1, page1);
+        if (EARLY && n > 2) look_up(2, page2);
+        page = EARLY ? page3 : page2;
         __syncthreads();
         request_direct(0, Even{});
         request(0);
         put(0, Even{});
         if (EARLY && n > 1) request(1);
     }
-    __builtin_amdgcn_s_waitcnt(0x0F70);           // vmcnt(0): what goes to shared memory directly is there
+    // what goes to shared memory directly is there: nothing is on its way but what was asked for after it
+    if (!E8 && EARLY && n > 1) __builtin_amdgcn_s_waitcnt(0x0F70 | (VK & 15) | (VK >> 4 << 14));
+    else if (!E8) __builtin_amdgcn_s_waitcnt(0x0F70);
     __syncthreads();
     auto step = [&](int i, auto odd_tile) {
         using Next = Odd<!decltype(odd_tile)::value>;
@@ -415,15 +457,15 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         if (EARLY && i + 1 < n) request_direct(i + 1, Next{});
         compute(i, odd_tile, [&] {
             if (EARLY) {
-                if (i + 3 < n) look_up(i + 3);
-                if (i + 4 < n) ask(i + 4);
+                if (i + 3 < n) look_up(i + 3, page);
+                if (i + 4 < n) page = ask(i + 4);
             } else {
                 if (i + 1 < n) {
                     request_direct(i + 1, Next{});
                     request(i + 1);
                 }
-                if (i + 2 < n) look_up(i + 2);
-                if (i + 3 < n) ask(i + 3);
+                if (i + 2 < n) look_up(i + 2, page);
+                if (i + 3 < n) page = ask(i + 3);
             }
         }, [&] {
             if (i + 1 < n) put(i + 1, Next{});
@@ -464,7 +506,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     if (my >= nr) return;
     const bool empty = m == -INFINITY;
     const float v_scale = E8 && C.v_scale ? C.v_scale[kvh] : 1.f;
-    if (P.pieces > 1) {
+    if (pieces) {
         float *place = scratch + (((size_t)b * P.tiles + tile) * C.n_kv_heads + kvh) * P.pieces * ROWS * (HD + 2) + (size_t)piece * ROWS * (HD + 2);
         float *dst = place + (size_t)(32 * part + r32) * HD;
 #pragma unroll
@@ -503,12 +545,18 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const 
     const int rr = 16 * slice + (threadIdx.x >> 4), part = threadIdx.x & 15, r = tile * ROWS + rr;
     if (r >= s.n * A.G) return;
     const float c2 = A.attn.scale * 1.4426950408889634f * (E8 && C.k_scale ? C.k_scale[kvh] : 1.f);
+    const int row0 = tile * ROWS;
+    const int last = row0 + ROWS < s.n * A.G ? row0 + ROWS - 1 : s.n * A.G - 1;
+    const int steps = steps_of<KT>(A.attn, s.len - s.n + row0 / A.G, s.len - s.n + last / A.G, s.len).steps;
+    const int size = ROWS == 64 ? even_size(steps, P.pieces) : *size_place(A, P, const_cast<float *>(scratch), ROWS, HD);
+    const int pieces = (steps + size - 1) / size;
+    if (pieces <= 1) return;
     const float *place = scratch + (((size_t)b * P.tiles + tile) * C.n_kv_heads + kvh) * P.pieces * ROWS * (HD + 2);
     float mx = -INFINITY, sum = 0.f, o[NE];
-    for (int q = 0; q < P.pieces; ++q) mx = fmaxf(mx, place[(size_t)q * ROWS * (HD + 2) + (size_t)ROWS * HD + 2 * rr]);
+    for (int q = 0; q < pieces; ++q) mx = fmaxf(mx, place[(size_t)q * ROWS * (HD + 2) + (size_t)ROWS * HD + 2 * rr]);
 #pragma unroll
     for (int e = 0; e < NE; ++e) o[e] = 0.f;
-    for (int q = 0; q < P.pieces; ++q) {
+    for (int q = 0; q < pieces; ++q) {
         const float *p = place + (size_t)q * ROWS * (HD + 2);
         const float2 ml = *reinterpret_cast<const float2 *>(p + (size_t)ROWS * HD + 2 * rr);
         const float f = ml.x == -INFINITY ? 0.f : exp2_((ml.x - mx) * c2);
@@ -527,15 +575,18 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const 
 // Rows of a workgroup: 64 (four waves, keys halved between them), 128 (four waves) or 256 (eight)
 int tile_rows(long rows) { return rows <= 64 ? 64 : (rows <= 128 ? 128 : 256); }
 
-// Pieces: as many as find a place on the device (two workgroups of four waves on a compute unit, one of eight), while a piece keeps
-// four tiles of the longest sequence that the table allows.  Twice as many for up to 64 rows, whose time is that of the
-// longest sequence.
+// Two workgroups of four waves find a place on a compute unit, one of eight.  Where the row tiles are few, their positions are cut into
+// pieces of four tiles at least of the longest sequence that the table allows: for 64 rows into as many as give four workgroups a
+// compute unit; for 128 into three rounds' worth, twice that for the longest (32 caches of up to 32767 positions, 32 rows of 4 heads
+// each: one round 632 us, two 491, three 363; whole sequences 650); for 256 into one round's.
 Cut cut_of(long rows, int B, int n_kv_heads, long positions, int nCU) {
     Cut c;
     const int per = tile_rows(rows);
+    const long items = rows > 0 ? (rows + per - 1) / per * B * n_kv_heads : 0, longest = positions / (4 * KT);
     c.tiles = (int)((rows + per - 1) / per);
-    const long items = (long)c.tiles * B * n_kv_heads, longest = positions / (4 * KT);
-    long pieces = items > 0 ? (per == 64 ? 4 : (per == 128 ? 2 : 1)) * (long)nCU / items : 1;
+    c.slots = (per == 128 ? 6 : 1) * (nCU > 0 ? nCU : 1);
+    long pieces = 1;
+    if (items > 0) pieces = per == 64 ? 4 * (long)c.slots / items : (items < c.slots ? (2 * (long)c.slots + items - 1) / items : 1);
     if (pieces > longest) pieces = longest;
     c.pieces = pieces < 1 ? 1 : (int)pieces;
     return c;
@@ -570,7 +621,7 @@ bool prompt_takes(long rows, int head_dim) { return rows > 32 && head_dim <= 128
 
 size_t prompt_scratch_floats(long rows, int B, int n_kv_heads, long positions, int head_dim, int nCU) {
     const Cut c = cut_of(rows, B, n_kv_heads, positions, nCU);
-    return c.pieces > 1 ? (size_t)c.tiles * B * n_kv_heads * c.pieces * tile_rows(rows) * (head_dim + 2) : 0;
+    return c.pieces > 1 ? pieces_floats(B, c, n_kv_heads, tile_rows(rows), head_dim) + 4 : 0;
 }
 
 hipError_t launch_prompt_attention(const Attend &a, float *scratch, int nCU, hipStream_t st) {
