@@ -63,7 +63,7 @@ __device__ __forceinline__ int *size_place(const Attend &A, const Cut &P, float 
     return reinterpret_cast<int *>(scratch + pieces_floats(A.rows.B, P, A.cache.n_kv_heads, rows, HD));
 }
 
-// Where the positions of 64 rows are cut: into as many parts for each sequence (32 caches of up to 8000 positions of 8 bits: 96 us; cut as
+// Where the positions of 64 rows are cut: into as many parts for each sequence (32 caches of up to 8000 positions of 8 bits: 95 us; cut as
 // below 117 to 126, whose few longer parts come in rounds)
 __device__ __forceinline__ int even_size(int steps, int pieces) {
     const int size = (steps + pieces - 1) / pieces;
@@ -615,7 +615,7 @@ void launch_hd(const Attend &a, const Cut &c, int rows, float *scratch, hipStrea
 }  // namespace
 
 // From 33 rows of a key head.  64 rows here / in paged_attention.hip's kernel (four waves, 16 rows each): 64 caches of up to 32767
-// positions, bf16, 672 / 704 us; 32 of up to 8000, e4m3, 96 / 135.  32 rows there: 469, bf16.  (Heads of 256 stay there: their sums and
+// positions, bf16, 640 to 680 / 704 us; 32 of up to 8000, e4m3, 95 / 135.  32 rows there: 469, bf16.  (Heads of 256 stay there: their sums and
 // queries would not fit a wave's registers here.)
 bool prompt_takes(long rows, int head_dim) { return rows > 32 && head_dim <= 128; }
 
