@@ -454,7 +454,8 @@ int mrp_cache_append(mrp_ctx *ctx, void *stream, long n_rows, const mrp_new_rows
 /* Attention of the batch's new rows over the cache, which holds their own keys and values too (mrp_cache_append first):
  *   out = softmax(scale q k^T) v over the positions j that the row, at position p, sees:
  *   j <= p (causal) or j < kv_len[b] (a block whose rows all see each other), and, with a window, j > p - window or
- *   j < n_sink.  A row that sees nothing (padding, pages that are not there) has out = 0 and lse = -inf.
+ *   j < n_sink.  A row that sees nothing (padding, pages that are not there) has out = 0 and lse = -inf;
+ *   one with a score that is NaN or +inf has NaN in out and in lse, one whose scores are all -inf NaN and -inf.
  * What lies in places that no row of a sequence sees, or only others than this row, does not reach its output, whatever it
  * is; a visible value that is not finite makes the outputs that take it not finite.  Scores and sums are kept in 32 bits, the
  * softmax weights as the two leading terms of dtype where max_new tokens make up to 32 rows of a key head, as one rounded to

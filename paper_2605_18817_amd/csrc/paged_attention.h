@@ -82,6 +82,12 @@ __device__ __forceinline__ uint32_t seen_bits(int p, int key0, int len, const mr
     return seen;
 }
 
+// A row's largest score starts at -inf, which is what it keeps where it sees nothing; whoever sees a position raises it to LOWEST at
+// least, so that scores that are no numbers (the maximum passes them over) or -inf leave a sum of NaN or 0 and not an empty row.
+constexpr float LOWEST = -3.4028234663852886e38f;
+// The reference of the weights in units of log 2: finite, so that a score of -inf weighs nothing
+__device__ __forceinline__ float reference(float m, float c2) { return fmaxf(m * c2, LOWEST); }
+
 // The larger of a lane's value and that of the lane 32 (16) from it
 __device__ __forceinline__ float max_halves(float x) {
     const auto p = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

@@ -289,9 +289,11 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
                     }
                 }
 
+                float mx = fmaxf(m, LOWEST);
                 if (partial) {
                     // scores of positions that a row does not see are dropped
-                    const uint32_t seen = (seen_bits(pos, key0, s.len, A.attn) & there) >> (8 * g);
+                    const uint32_t all = seen_bits(pos, key0, s.len, A.attn) & there, seen = all >> (8 * g);
+                    mx = all ? mx : m;
 #pragma unroll
                     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -300,11 +302,10 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
 
                 // softmax of the step, and the weights as operands: the leading 16-bit term and the next
                 u32x4 ph, pl;
-                float mx = m;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
                 mx = max_halves(max_quarters(mx));
-                const float ref = mx == -INFINITY ? 0.f : mx * c2;
+                const float ref = reference(mx, c2);
                 if (__any(mx > m)) {
                     const float alpha = exp2_(m * c2 - ref);
                     l *= alpha;

@@ -349,18 +349,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         four_ahead<NT * NC>();
         after_scores();
         const bool partial = is_partial(key0, th0, th1);
+        float mx = LOWEST;
         if (partial) {
+            uint32_t any = 0;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int tt = KH == 2 ? half : t;
-                const uint32_t seen = (seen_bits(pos, key0 + 32 * tt, s.len, A.attn) & (tt ? th1 : th0)) >> (8 * h);
+                const uint32_t all = seen_bits(pos, key0 + 32 * tt, s.len, A.attn) & (tt ? th1 : th0), seen = all >> (8 * h);
+                any |= all;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) sc[t][i] = (seen >> (16 * (i >> 3) + (i & 7))) & 1u ? sc[t][i] : -INFINITY;
             }
+            mx = any ? LOWEST : -INFINITY;
         }
-        float mx = sc[0][0];
 #pragma unroll
-        for (int i = 1; i < 16 * NT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
+        for (int i = 0; i < 16 * NT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
         mx = max_halves(mx);
         // the sums are brought to a new reference where a score is more than a factor of 2^8 above the old one
         if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx > m))) {
@@ -371,7 +374,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
             for (int d = 0; d < ND; ++d) acc[d] *= alpha;
         }
-        const float ref = m == -INFINITY ? 0.f : m * c2;
+        const float ref = reference(m, c2);
         u32x4 p[2 * NT];                          // the weights of 16 keys each, rounded to 16 bits
         float sum = 0.f;
 #pragma unroll
