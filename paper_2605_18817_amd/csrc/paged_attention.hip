@@ -307,7 +307,7 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
                 mx = max_halves(max_quarters(mx));
                 const float ref = reference(mx, c2);
                 if (__any(mx > m)) {
-                    const float alpha = exp2_(m * c2 - ref);
+                    const float alpha = exp2_(reference(m, c2) - ref);   // (exactly 1 where the row's maximum stays)
                     l *= alpha;
 #pragma unroll
                     for (int e = 0; e < NE; ++e) acc[e] *= alpha;
