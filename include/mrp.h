@@ -259,7 +259,8 @@ int mrp_build_candidates(mrp_ctx *ctx, void *stream, int B, int K, const int32_t
  *   MRP_FLAG_POSITION    a row's position outside [0, n_pos) of the rotation table: clamped
  *   MRP_FLAG_ROWS        cu_rows outside [0, n_rows], decreasing, or more than max_new apart: clamped
  *   MRP_FLAG_KV_LEN      kv_len[b] outside [0, max_pages * page_size]: clamped
- *   MRP_FLAG_PAGE        a page number outside [0, n_pages): its positions are neither written nor seen
+ *   MRP_FLAG_PAGE        a page number outside [0, n_pages): its positions are neither written nor seen (pages that no row
+ *                        writes or sees, behind a window for instance, may have any)
  * mrp_poll_error waits for `stream` (hipStreamSynchronize: not for use under stream capture), returns the
  * bits set since the last poll (0 = none) and clears them, or a negative status; mrp_last_error then
  * names the conditions. */

@@ -148,6 +148,8 @@ __device__ __forceinline__ void store_row(const Attend &A, long row, int head, i
 struct Steps {
     int first, s_steps, steps, low, high;
 };
+// Does any of these rows see position j?  (Pages of others are not looked at: behind a window they may be another sequence's, or none.)
+__device__ __forceinline__ bool any_sees(const Steps &t, int n_sink, int j) { return j < t.high && (j >= t.low || j < n_sink); }
 template <int STEP>
 __device__ __forceinline__ Steps steps_of(const mrp_attn &a, int p_first, int p_last, int len) {
     Steps t;

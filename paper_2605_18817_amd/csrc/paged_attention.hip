@@ -207,10 +207,10 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
             for (int e = 0; e < NE; ++e) acc[e] = f32x4{0.f, 0.f, 0.f, 0.f};
 
             auto key_of = [&](int u) { return (u < st.s_steps ? u : st.first + u - st.s_steps) * STEP; };
-            // the page of step u's positions (of position key + lane % 32, where pages end inside a step), or -1
+            // the page of step u's positions (of position key + lane % 32, where pages end inside a step; 0 where no row sees it)
             auto page_of = [&](int u) {
                 const int j = key_of(u) + (whole ? 0 : (lane & 31));
-                return j < high ? table[j / C.page_size] : 0;
+                return whole || any_sees(st, sink, j) ? table[j / C.page_size] : 0;
             };
             struct Raw {
                 u32x4 k[2][NL];

@@ -209,14 +209,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     // The first wave looks up the places of the piece's tile i: it asks for the page numbers a turn before it needs them
     auto ask = [&](int i) {
         const int j = key_of(begin + i) + lane;
-        return wave == 0 && j < st.high ? table[j / C.page_size] : -1;
+        return wave == 0 && any_sees(st, sink, j) ? table[j / C.page_size] : -1;
     };
     auto look_up = [&](int i, int page) {
         const int at = i & 3;
         if (wave == 0) {
             const int j = key_of(begin + i) + lane;
             const bool ok = page >= 0 && page < C.n_pages;
-            if (!ok && j < st.high) atomicOr(A.err_flag, ERR_PAGE);
+            if (!ok && any_sees(st, sink, j)) atomicOr(A.err_flag, ERR_PAGE);
             places[at][lane] = ok ? ((long)page * C.page_size + j % C.page_size) * pitch : 0;
             const unsigned long long all = __ballot(ok);
             if (lane == 0) {
