@@ -30,6 +30,17 @@ __device__ __forceinline__ uint32_t pack2(F16, float x, float y, float &rx, floa
     ry = y - (float)h[1];
     return __builtin_bit_cast(uint32_t, h);
 }
+// fp16 weights are carried as 2^SHIFT times themselves, through the sums as well: below 2^-14 its steps are 2^-24, whatever the weight,
+// and many small weights next to a large one would drop out of the product alone.  The largest is 2^10 then (up to 32 rows of a key head, in
+// two terms), or 2^7 to 2^15 where the reference may lag by 2^8; fp16 ends at 2^16.
+template <typename T, int BITS>
+struct Scaled {
+    static constexpr float SHIFT = __is_same(T, F16) ? BITS : 0, ONE = __is_same(T, F16) ? 1 << BITS : 1;
+};
+template <typename T>
+using Few = Scaled<T, 10>;
+template <typename T>
+using Many = Scaled<T, 7>;
 // four e4m3 values as 16-bit ones (exact in both types)
 __device__ __forceinline__ void widen(BF16, uint32_t v, uint32_t &lo, uint32_t &hi) {
     lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, false));
@@ -128,9 +139,9 @@ __device__ __forceinline__ Words<N> load_words(const char *p) {
     return r;
 }
 
-// A row's part: normalised, rounded, and its log-sum (m2: the reference in units of log 2)
+// A row's part: normalised, rounded, and its log-sum (m2: the reference in units of log 2; one: the weight there)
 template <typename T, int HD>
-__device__ __forceinline__ void store_row(const Attend &A, long row, int head, int part, bool empty, float m2, float sum, float v_scale,
+__device__ __forceinline__ void store_row(const Attend &A, long row, int head, int part, bool empty, float m2, float one, float sum, float v_scale,
                                           float (&o)[HD / 16]) {
     constexpr int NE = HD / 16;
     const float f = v_scale / sum;
@@ -141,7 +152,7 @@ __device__ __forceinline__ void store_row(const Attend &A, long row, int head, i
     for (int e = 0; e < NE; e += 2) w.w[e / 2] = empty ? 0u : pack2(T{}, o[e] * f, o[e + 1] * f, x, y);
 #pragma unroll
     for (int e = 0; e < NE / 2; ++e) dst[e] = w.w[e];
-    if (A.lse && part == 0) A.lse[row * A.attn.n_heads + head] = empty ? -INFINITY : m2 * 0.6931471805599453f + logf(sum);
+    if (A.lse && part == 0) A.lse[row * A.attn.n_heads + head] = empty ? -INFINITY : m2 * 0.6931471805599453f + logf(sum * (1.f / one));
 }
 
 // Steps of STEP positions for rows at p_first .. p_last of a sequence: [0, sink) in s_steps of them, [low, high) from step `first`

@@ -305,9 +305,9 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(sc[0][i], sc[1][i]));
                 mx = max_halves(max_quarters(mx));
-                const float ref = reference(mx, c2);
+                const float shift = Few<T>::SHIFT - reference(mx, c2);
                 if (__any(mx > m)) {
-                    const float alpha = exp2_(reference(m, c2) - ref);   // (exactly 1 where the row's maximum stays)
+                    const float alpha = exp2_(shift - (Few<T>::SHIFT - reference(m, c2)));   // (exactly 1 where the row's maximum stays)
                     l *= alpha;
 #pragma unroll
                     for (int e = 0; e < NE; ++e) acc[e] *= alpha;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; i += 2) {
-                        const float p0 = exp2_(fmaf(sc[t][i], c2, -ref)), p1 = exp2_(fmaf(sc[t][i + 1], c2, -ref));
+                        const float p0 = exp2_(fmaf(sc[t][i], c2, shift)), p1 = exp2_(fmaf(sc[t][i + 1], c2, shift));
                         float r0, r1, x, y;
                         sum += p0 + p1;
                         ph[2 * t + i / 2] = pack2(T{}, p0, p1, r0, r1);
@@ -444,7 +444,7 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
                 }
                 if (all) {
                     const int t = r / G;
-                    store_row<T, HD>(A, s.begin + t, kvh * G + r - t * G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
+                    store_row<T, HD>(A, s.begin + t, kvh * G + r - t * G, part, mx == -INFINITY, mx * c2, Few<T>::ONE, sum, v_scale, o);
                 } else {
                     float4 *dst = reinterpret_cast<float4 *>(place + (size_t)at * HD + NE * part);
 #pragma unroll
@@ -509,7 +509,7 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(const Attend 
         }
         for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor(sum, off);
         const int r = row0 + rr, t = r / A.G;
-        store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, sum, v_scale, o);
+        store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, Few<T>::ONE, sum, v_scale, o);
     }
 }
 

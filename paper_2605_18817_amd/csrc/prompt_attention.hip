@@ -365,21 +365,22 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
 #pragma unroll
         for (int i = 0; i < 16 * NT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
         mx = max_halves(mx);
-        // the sums are brought to a new reference where a score is more than a factor of 2^8 above the old one
-        if (__any((mx - m) * c2 > 8.f || (m == -INFINITY && mx > m))) {
+        // the sums are brought to a new reference where a weight would be more than 2^8 of the old one's unit
+        float shift = Many<T>::SHIFT - reference(m, c2);
+        if (__any(fmaf(mx, c2, shift) > 8.f + Many<T>::SHIFT || (m == -INFINITY && mx > m))) {
             const float top = fmaxf(m, mx);
             const float alpha = m == -INFINITY ? 0.f : exp2_((m - top) * c2);
             m = top;
             l *= alpha;
 #pragma unroll
             for (int d = 0; d < ND; ++d) acc[d] *= alpha;
+            shift = Many<T>::SHIFT - reference(m, c2);
         }
-        const float ref = reference(m, c2);
         u32x4 p[2 * NT];                          // the weights of 16 keys each, rounded to 16 bits
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16 * NT; i += 2) {
-            const float p0 = exp2_(fmaf(sc[i >> 4][i & 15], c2, -ref)), p1 = exp2_(fmaf(sc[i >> 4][(i & 15) + 1], c2, -ref));
+            const float p0 = exp2_(fmaf(sc[i >> 4][i & 15], c2, shift)), p1 = exp2_(fmaf(sc[i >> 4][(i & 15) + 1], c2, shift));
             float x, y;
             sum += p0 + p1;
             p[i >> 3][(i & 7) >> 1] = pack2(T{}, p0, p1, x, y);
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
             for (int k = 0; k < 4; ++k) w[k] = empty ? 0u : pack2(T{}, acc[d][i + k] * f, acc[d + ND / 2][i + k] * f, x, y);
             *reinterpret_cast<uint4 *>(A.out + at * HD + 2 * (32 * d + 2 * i + 4 * h)) = make_uint4(w[0], w[1], w[2], w[3]);
         }
-    if (A.lse && h == 0) A.lse[at] = empty ? -INFINITY : m * c2 * 0.6931471805599453f + logf(l);
+    if (A.lse && h == 0) A.lse[at] = empty ? -INFINITY : m * c2 * 0.6931471805599453f + logf(l * (1.f / Many<T>::ONE));
 }
 
 // Adds up a row tile's pieces in the order of their positions: 16 threads a row, 16 rows a workgroup
@@ -572,7 +573,7 @@ __global__ __launch_bounds__(256) void prompt_join_kernel(const Attend A, const 
         }
     }
     const int t = r / A.G;
-    store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, sum, E8 && C.v_scale ? C.v_scale[kvh] : 1.f, o);
+    store_row<T, HD>(A, s.begin + t, kvh * A.G + r - t * A.G, part, mx == -INFINITY, mx * c2, Many<T>::ONE, sum, E8 && C.v_scale ? C.v_scale[kvh] : 1.f, o);
 }
 
 // Rows of a workgroup: 64 (four waves, keys halved between them), 128 (four waves) or 256 (eight)
