@@ -33,14 +33,15 @@ __device__ __forceinline__ uint32_t pack2(F16, float x, float y, float &rx, floa
 // fp16 weights are carried as 2^SHIFT times themselves, through the sums as well: below 2^-14 its steps are 2^-24, whatever the weight,
 // and many small weights next to a large one would drop out of the product alone.  The largest is 2^10 then (up to 32 rows of a key head, in
 // two terms), or 2^7 to 2^15 where the reference may lag by 2^8; fp16 ends at 2^16.
-template <typename T, int BITS>
+// bf16 weights whose reference may lag are carried as 2^-8 times themselves: the sums end where those of weights of 1 would.
+template <int BITS>
 struct Scaled {
-    static constexpr float SHIFT = __is_same(T, F16) ? BITS : 0, ONE = __is_same(T, F16) ? 1 << BITS : 1;
+    static constexpr float SHIFT = BITS, ONE = BITS < 0 ? 1.f / (1 << -BITS) : 1 << BITS;
 };
 template <typename T>
-using Few = Scaled<T, 10>;
+using Few = Scaled<__is_same(T, F16) ? 10 : 0>;
 template <typename T>
-using Many = Scaled<T, 7>;
+using Many = Scaled<__is_same(T, F16) ? 7 : -8>;
 // four e4m3 values as 16-bit ones (exact in both types)
 __device__ __forceinline__ void widen(BF16, uint32_t v, uint32_t &lo, uint32_t &hi) {
     lo = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.0f, false));
