@@ -440,7 +440,7 @@ typedef struct {
     int n_kv_heads, head_dim;
     int n_pages, page_size;    /* n_pages * page_size < 2^31 */
     const int32_t *page_table; /* [B][max_pages] */
-    int max_pages;             /* max_pages * page_size < 2^31 */
+    int max_pages;             /* max_pages * page_size <= 2^31 - 4096 */
     const float *k_scale, *v_scale;
 } mrp_paged_cache;
 

@@ -373,6 +373,7 @@ bool for_types(int x, int y, Fn f) {
 }
 
 constexpr long MAX_ROWS = 1L << 24;
+constexpr long MAX_POSITIONS = (1L << 31) - 4096;   // of a sequence: tiles are looked up ahead of the last one, with positions in an int
 constexpr long MAX_THREADS = 0xffffff00L;   // of one launch
 
 // What all calls on a mrp_qk check; the heads that are given are checked by their callers
@@ -451,7 +452,7 @@ int check_cache(mrp_ctx *c, const char *what, const mrp_paged_cache *k) {
     if (k->head_dim != 64 && k->head_dim != 128 && k->head_dim != 256)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: head_dim %d is none of 64, 128, 256", what, k->head_dim);
     if (k->n_kv_heads < 1 || k->n_kv_heads > 1024 || k->n_pages < 1 || k->page_size < 1 || k->max_pages < 1 ||
-        (long)k->n_pages * k->page_size > 0x7fffffffL || (long)k->max_pages * k->page_size > 0x7fffffffL)
+        (long)k->n_pages * k->page_size > 0x7fffffffL || (long)k->max_pages * k->page_size > MAX_POSITIONS)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %d kv heads, %d pages of %d, %d a sequence out of range", what, k->n_kv_heads,
                         k->n_pages, k->page_size, k->max_pages);
     if (!aligned16(k->k_pages) || !aligned16(k->v_pages)) return ctx_fail(c, MRP_ERR_ALIGN, "%s: pages must be 16-byte aligned", what);
