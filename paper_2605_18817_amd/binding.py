@@ -208,6 +208,13 @@ def _rows(t, name: str, shape, dtype: int, device: int):
     return t.data_ptr(), (row if n > 1 else heads * head_dim)
 
 
+def _int(value: int, name: str) -> int:
+    """A size as the library's ints hold it (ctypes would keep the low 32 bits of another)."""
+    if not 0 <= value < 2 ** 31:
+        raise MrpError(f"{name}={value} out of range")
+    return value
+
+
 def _device_of(*tensors) -> Optional[int]:
     """The one device that the tensors (None: not given) are on."""
     found = {t.get_device() for t in tensors if t is not None}
@@ -328,6 +335,7 @@ class NewRows:
 
     def __init__(self, kv_len, max_new: int, cu_rows=None):
         _dtypes()
+        _int(max_new, "max_new")
         self.B = B = kv_len.shape[0]
         self.tensors = (kv_len, cu_rows)
         self.device = dev = _device_of(*self.tensors)
@@ -365,8 +373,7 @@ class AttnCfg:
     n_sink: int = 0
 
     def __post_init__(self):
-        if not (0 <= self.window < 2 ** 31 and 0 <= self.n_sink < 2 ** 31):
-            raise MrpError(f"window={self.window} n_sink={self.n_sink} out of range")
+        _int(self.window, "window"), _int(self.n_sink, "n_sink")
 
 
 class StepIO:
@@ -562,6 +569,7 @@ class MrpContext:
     def rope_table(self, n_pos: int, rotary_dim: int, theta: float):
         """cos and sin of every position and pair: fp32 [n_pos][rotary_dim / 2][2]."""
         import torch
+        _int(n_pos, "n_pos"), _int(rotary_dim, "rotary_dim")
         out = torch.empty((n_pos, rotary_dim // 2, 2), dtype=torch.float32, device=f"cuda:{self.device}")
         self._check(self.lib.mrp_rope_table(self._h, self._raw_stream(), n_pos, rotary_dim, theta, out.data_ptr()), "mrp_rope_table")
         return out

@@ -3,6 +3,7 @@ device (a block of zeros stands in for a context)."""
 import ctypes as C
 
 import pytest
+import torch
 
 import paper_2605_18817_amd as mrp
 from paper_2605_18817_amd import binding as bd
@@ -30,3 +31,14 @@ def test_the_largest_table_is_taken():
     cache = bd._PagedCache(A, A, 1, 2, 128, 1, 4096, A, 2 ** 19 - 1, None, None)          # 2^31 - 4096 positions
     qk = bd._Qk(8, 2, 128, 64, 1, 1, 1, 1e-6, A, A, A, 100)
     assert lib.mrp_cache_append(ctx, None, 0, bd._NewRows(3, 4, A, A), qk, A, 1024, A, 256, A, 256, cache, A) == 0
+
+
+def test_sizes_that_an_int_does_not_hold():
+    """ctypes keeps the low 32 bits of a size: what does not fit is refused, not taken for another."""
+    with pytest.raises(mrp.MrpError, match="max_new"):
+        mrp.NewRows(torch.zeros(3, dtype=torch.int32), 2 ** 32 + 1)
+    ctx = object.__new__(mrp.MrpContext)                   # (nothing of a context is looked at before)
+    with pytest.raises(mrp.MrpError, match="n_pos"):
+        ctx.rope_table(2 ** 32 + 8, 64, 1e4)
+    with pytest.raises(mrp.MrpError, match="rotary_dim"):
+        ctx.rope_table(8, 2 ** 32 + 64, 1e4)
