@@ -22,7 +22,7 @@
 namespace mrp {
 
 int check_new_rows(mrp_ctx *c, const char *what, long n_rows, const mrp_new_rows *r);
-int check_cache(mrp_ctx *c, const char *what, const mrp_paged_cache *k);
+int check_cache(mrp_ctx *c, const char *what, const mrp_paged_cache *k, int B);
 int check_context_device(mrp_ctx *c, const char *what);
 
 namespace {
@@ -573,7 +573,7 @@ int mrp_paged_attention(mrp_ctx *c, void *stream, long n_rows, const mrp_new_row
     if (!c) return MRP_ERR_NULL;
     if (!rows || !cache || !attn) return ctx_fail(c, MRP_ERR_NULL, "%s: NULL pointer", what);
     CHECK(check_new_rows(c, what, n_rows, rows));
-    CHECK(check_cache(c, what, cache));
+    CHECK(check_cache(c, what, cache, rows->B));
     if (attn->n_heads < 1 || attn->n_heads > 1024 || attn->n_heads % cache->n_kv_heads)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %d heads over %d key heads", what, attn->n_heads, cache->n_kv_heads);
     if (n_rows * attn->n_heads > (1L << 28) || most_rows(n_rows, *rows, attn->n_heads / cache->n_kv_heads) > (1L << 22) ||

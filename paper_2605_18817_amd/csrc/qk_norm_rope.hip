@@ -445,8 +445,8 @@ int check_new_rows(mrp_ctx *c, const char *what, long n_rows, const mrp_new_rows
     return MRP_OK;
 }
 
-int check_cache(mrp_ctx *c, const char *what, const mrp_paged_cache *k) {
-    if (!k->k_pages || !k->v_pages || !k->page_table) return ctx_fail(c, MRP_ERR_NULL, "%s: the cache has a NULL pointer", what);
+int check_cache(mrp_ctx *c, const char *what, const mrp_paged_cache *k, int B) {
+    if (!k->k_pages || !k->v_pages || (B > 0 && !k->page_table)) return ctx_fail(c, MRP_ERR_NULL, "%s: the cache has a NULL pointer", what);
     if (k->dtype != MRP_DTYPE_BF16 && k->dtype != MRP_DTYPE_F16 && k->dtype != MRP_DTYPE_E4M3)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: cache type %d", what, k->dtype);
     if (k->head_dim != 64 && k->head_dim != 128 && k->head_dim != 256)
@@ -566,7 +566,7 @@ int mrp_cache_append(mrp_ctx *c, void *stream, long n_rows, const mrp_new_rows *
     if (!rows || !qk || !cache) return ctx_fail(c, MRP_ERR_NULL, "%s: NULL pointer", what);
     CHECK(check_qk(c, what, n_rows, qk));
     CHECK(check_new_rows(c, what, n_rows, rows));
-    CHECK(check_cache(c, what, cache));
+    CHECK(check_cache(c, what, cache, rows->B));
     if (qk->head_dim != cache->head_dim || qk->n_kv_heads != cache->n_kv_heads)
         return ctx_fail(c, MRP_ERR_SHAPE, "%s: %d key heads of %d, but the cache has %d of %d", what, qk->n_kv_heads, qk->head_dim,
                         cache->n_kv_heads, cache->head_dim);

@@ -42,3 +42,15 @@ def test_sizes_that_an_int_does_not_hold():
         ctx.rope_table(2 ** 32 + 8, 64, 1e4)
     with pytest.raises(mrp.MrpError, match="rotary_dim"):
         ctx.rope_table(8, 2 ** 32 + 64, 1e4)
+
+
+def test_batches_of_no_sequence():
+    """B = 0 is a batch like any other; the table of such a batch has no address."""
+    lib, ctx = mrp.load_library(), C.cast(C.create_string_buffer(1 << 14), C.c_void_p)
+    qk = bd._Qk(8, 2, 128, 64, 1, 1, 1, 1e-6, A, A, A, 100)
+    cache = bd._PagedCache(A, A, 1, 2, 128, 1, 16, None, 5, None, None)
+    for n in (0, 12):                                      # (rows of no sequence are left as they are)
+        for cu in (None, A):
+            rows = bd._NewRows(0, 4, cu, None)
+            assert lib.mrp_cache_append(ctx, None, n, rows, qk, A, 1024, A, 256, A, 256, cache, A) == 0
+            assert lib.mrp_paged_attention(ctx, None, n, rows, cache, bd._Attn(8, 1, 0.1, 1, 0, 0), A, 1024, A, None, None, 0) == 0
