@@ -210,7 +210,7 @@ __global__ __launch_bounds__(64 * WAVES, HD <= 128 ? 2 : 1) void paged_attention
             // the page of step u's positions (of position key + lane % 32, where pages end inside a step; 0 where no row sees it)
             auto page_of = [&](int u) {
                 const int j = key_of(u) + (whole ? 0 : (lane & 31));
-                return whole || any_sees(st, sink, j) ? table[j / C.page_size] : 0;
+                return j < high && (whole || j >= low || j < sink) ? table[j / C.page_size] : 0;
             };
             struct Raw {
                 u32x4 k[2][NL];

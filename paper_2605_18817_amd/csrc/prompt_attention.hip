@@ -208,11 +208,11 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
     };
     // The first wave looks up the places of the piece's tile i: it asks for the page numbers a turn before it needs them
     auto ask = [&](int i) {
-        const int j = key_of(begin + i) + lane;
+        const int j = key_of(begin + i) + (anew(threadIdx.x) & 63);
         return wave == 0 && any_sees(st, sink, j) ? table[j / C.page_size] : -1;
     };
     auto look_up = [&](int i, int page) {
-        const int at = i & 3;
+        const int lane = anew(threadIdx.x) & 63, at = i & 3;
         if (wave == 0) {
             const int j = key_of(begin + i) + lane;
             const bool ok = page >= 0 && page < C.n_pages;
