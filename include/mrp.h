@@ -459,8 +459,11 @@ int mrp_cache_append(mrp_ctx *ctx, void *stream, long n_rows, const mrp_new_rows
  *   one with a score that is NaN or +inf has NaN in out and in lse, one whose scores are all -inf NaN and -inf.
  * What lies in places that no row of a sequence sees, or only others than this row, does not reach its output, whatever it
  * is; a visible value that is not finite makes the outputs that take it not finite.  Scores and sums are kept in 32 bits, the
- * softmax weights as the two leading terms of dtype where max_new tokens make up to 32 rows of a key head, as one rounded to
- * dtype for more (fp16: to multiples of 2^-34 of the row's largest, of 2^-31 for more rows, or finer).
+ * softmax weights as the two leading terms of dtype where max_new tokens make up to 32 rows of a key head or
+ * head_dim is 256, as one rounded to dtype otherwise (fp16: to multiples of 2^-34 of the row's largest, of 2^-31 where as one, or finer).
+ * The form that a sequence's rows take goes by max_new: single tokens in a batch with a prompt are worked on like the prompt, at many times
+ * the time of a call of their own.
+ * n_rows * n_heads <= 2^28; min(max_new, n_rows) * n_heads / n_kv_heads and B * n_kv_heads <= 2^22.
  * q, out: dtype BF16 or F16, the cache's where that is not E4M3; out [n_rows][n_heads][head_dim] dense; lse fp32
  * [n_rows][n_heads]: log of the sum of exp(scale q k), or NULL.  scratch: mrp_paged_attention_scratch_bytes, 16-byte aligned, of the
  * caller's; it holds nothing between calls, and calls that may overlap in time (two graphs on two streams) need one each. */

@@ -115,7 +115,8 @@ template <int N>
 struct Words {
     uint32_t w[N];
 };
-// (ONCE: nobody else asks for them)
+// (ONCE: past the caches, where one workgroup takes all rows of a key head.  Sequences that share pages do ask again: 64 tokens over the same
+// 16384 positions 440 us, 291 through the caches, against 381 and 406 for 64 caches of their own, four rows each)
 template <bool ONCE>
 __device__ __forceinline__ u32x4 load_16(const char *p) {
     const u32x4 *q = reinterpret_cast<const u32x4 *>(p);

@@ -15,7 +15,7 @@
 // goes through shared memory until the waves of a workgroup, which take the steps of a sequence in turn, add up.
 //
 // Bound by the memory: a wave asks for 16 KB a step (heads of 128, 16 bits) and two waves share a SIMD.  64 caches of up to 32767
-// positions, 8 key heads of 128: 2.1 GB in 374 us, 5.6 TB/s (pages of one position 5.3); of 8 bits 4.4, whose 128 bytes a position lie
+// positions, 8 key heads of 128: 2.1 GB in 373 us, 5.7 TB/s (pages of one position 5.3); of 8 bits 4.5, whose 128 bytes a position lie
 // 1 KB apart; of 64 entries, 12 key heads, 4.9.
 #include "paged_attention.h"
 

@@ -11,8 +11,8 @@
 // their lanes.  Values are turned on their way into shared memory: entry d of all keys in row d / 2, the odd entries' rows behind the
 // even ones', so that a lane ends up with neighbouring entries of its output row.
 //
-// Two prompts of 4096 and 3565 rows behind 3987 and 2190 positions, 32 heads of 128 over 8: 637 GFLOP in 736 us, 870 TFLOP/s.  A tile costs a
-// wave 1024 cycles of the matrix core and about as many of the vector unit, 2740 in all for each of the two waves of a SIMD: within
+// Two prompts of 4096 and 3565 rows behind 3987 and 2190 positions, 32 heads of 128 over 8: 637 GFLOP in 733 us, 870 TFLOP/s.  A tile costs a
+// wave 1024 cycles of the matrix core and about as many of the vector unit, 2800 in all for each of the two waves of a SIMD: within
 // a wave they follow each other.  256 rows a workgroup rather than 128: 749 against 826 us, whose tiles are fetched and turned twice as often.
 #include "paged_attention.h"
 
@@ -457,7 +457,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_attention_kernel(const Atte
         // The next tile is asked for while the scores' products are under way, and its values are put in place ahead of the second
         // product: what a wave waits for is covered by what its matrix core does meanwhile.  EARLY: values (and keys of 8 bits) are
         // asked for a tile before that, since a tile's work is shorter than the memory takes; keys that go to shared memory
-        // directly at the tile's begin
+        // directly at the tile's begin.  The compiler waits for more than that: where the branches below join paths with different
+        // numbers of requests it waits for all (16 bits: ahead of an even tile's first product, and of an odd tile's page numbers
+        // and values; 8 bits: at the page number), so that less than a tile's work covers them
         if (EARLY && i + 1 < n) request_direct(i + 1, Next{});
         compute(i, odd_tile, [&] {
             if (EARLY) {
