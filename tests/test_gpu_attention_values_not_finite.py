@@ -16,14 +16,11 @@ def ctx():
     c.close()
 
 
-@pytest.mark.parametrize("value", [NAN, INF, -INF])
-@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("form,value", [(f, v) for f in FORMS for v in (NAN, INF, -INF) if v != v or f[6] != "e4m3"])     # (8 bits have no infinity)
 @pytest.mark.parametrize("back", [1, 3, 40, 70])
 def test_values(ctx, form, value, back):
     """Position kv_len - back of every sequence, entry 5 of the last key head: the rows before it are as if it were any value."""
     new, lens, H, Hkv, hd, dtype, cache = form
-    if cache == "e4m3" and value in (INF, -INF):
-        pytest.skip("8 bits have no infinity")
     batch = ref.Batch(new, lens, 16)
     g = torch.Generator(device="cuda").manual_seed(4)
     pages = [torch.randn((batch.n_pages, 16, Hkv, hd), generator=g, device="cuda").to(T[cache]) for _ in range(2)]
